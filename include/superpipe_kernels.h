@@ -139,6 +139,72 @@ int spk_gelu_bwd(void* stream, const uint16_t* dz, uint16_t* u, size_t n);
  * scratch: 256 * n floats.  n and ld even. */
 int spk_colsum_bf16(void* stream, const uint16_t* src, int ld, int T, int n, float* scratch, float* out);
 
+/* ---- packed batches: requests of different lengths ----
+ * A batch of n requests (1 <= n <= 4096) has its rows one behind the other: request r has the rows
+ * cu[r] .. cu[r+1]-1 of the T rows of a buffer (cu int32 [n+1], ascending, cu[n] <= T; requests without rows are
+ * allowed).  cu, lengths, tables and slots are device arrays, so that a step needs nothing from the host and can be captured;
+ * int32 and fp32 arrays need the alignment of their type only (scales: 8 bytes).  Whatever those arrays hold, the calls
+ * stay inside the buffers they are given.  Rows that belong to no request are left as they were. */
+
+/* One step's bookkeeping: request r, which has cached[r] positions already (cached == NULL: none has), gets lens[r] >= 0 new ones.
+ *   cu[0] = 0, cu[r+1] = cu[r] + lens[r];  kv_len[r] = cached[r] + lens[r]           (int32 [n+1], [n])
+ *   a request owns ceil(positions / block_size) blocks, named in order by its row of table int32 [n, max_blocks]: the rows
+ *   hold the blocks of the cached positions, the call adds the new ones, taking free_blocks [n_free] from the front in
+ *   the order of the requests
+ *   slots int32 [max_tokens]: slots[cu[r]+i] = table[r][p / block_size] * block_size + p % block_size, p = cached[r] + i;
+ *   -1 behind the last row
+ *   info int32 [4] = {rows, blocks taken, longest lens[r], 0}.
+ * What does not fit is not carried out at all: no rows (cu = 0, slots = -1), kv_len = cached, table as it was, and info[3] names
+ * the reasons, summed: 1 more rows than max_tokens, 2 more blocks than n_free, 4 a request past max_blocks, 8 a negative
+ * length (info[0..2] count all the same, negative lengths as 0).
+ * block_size 16, 32 or 64; max_blocks * block_size <= 2^30; 1 <= max_tokens <= 2^30; free_blocks may be NULL with n_free == 0;
+ * kv_len must not be cached (hand the two arrays over in turn). */
+int spk_batch_plan(void* stream, const int32_t* lens, const int32_t* cached, const int32_t* free_blocks, int n_free,
+                   int32_t* table, int max_blocks, int32_t* cu, int32_t* kv_len, int32_t* slots, int max_tokens,
+                   int32_t* info, int n, int block_size);
+
+/* spk_attention inside each request: row i attends the rows of its own request (causal != 0: up to itself).
+ * qkv bf16 [T, (Hq+2Hkv)*hd], o bf16 [T, Hq*hd] (not the same memory), lse fp32 [Hq, T] or NULL.  hd in {64,80,128}.
+ * A tile of 64 keys is worked as a whole: a key or value that is not finite may reach rows of its request up to 63 positions before
+ * it; other requests' rows never. */
+int spk_attention_packed(void* stream, const uint16_t* qkv, const int32_t* cu, uint16_t* o, float* lse, int n, int T,
+                         int Hq, int Hkv, int hd, int causal);
+
+/* Its backward: o and lse as the forward left them, dO bf16 [T, Hq*hd]; dqkv bf16 (layout of qkv) receives dq, dk, dv, the
+ * gradients of a key/value head summed over the query heads that share it (fixed order, no atomics).  scratch:
+ * spk_attention_packed_bwd_scratch_bytes bytes (the fp32 row sums of dO * O). */
+size_t spk_attention_packed_bwd_scratch_bytes(int T, int Hq);
+int spk_attention_packed_bwd(void* stream, const uint16_t* qkv, const int32_t* cu, const uint16_t* o, const uint16_t* dO,
+                             const float* lse, void* scratch, uint16_t* dqkv, int n, int T, int Hq, int Hkv, int hd,
+                             int causal);
+
+/* A key/value cache in 8 bits, one layer's: a pool of blocks of block_size (16, 32, 64) tokens,
+ *   k8 [blocks][Hkv][block_size][hd], v8 [blocks][Hkv][hd][block_size]: e4m3 (one byte, no infinities);
+ *   scales fp32 [blocks][Hkv][2]: what a block's key and value codes are multiplied with, powers of two.
+ * hd 64 or 128; blocks * block_size <= 2^31 - 1.
+ *
+ * Append: the key and value parts of row t of qkv bf16 [T, (Hq+2Hkv)*hd] go to slot slots[t] (block slots[t] / block_size,
+ * position slots[t] % block_size; outside the pool: the row is skipped).  Rows of one block have to lie close together, none more
+ * than 64 rows behind the one before it, which they do as spk_batch_plan deals them; they are stored in runs of
+ * consecutive slots, in the order of the rows.  A block's scale is the smallest 2^e,
+ * e >= -126, with all its finite |x| <= 448 * 2^e; a run that begins inside a block keeps what lies in front of it, re-coded
+ * if the scale has to grow, and what lies behind it in the block counts as empty.  Values are rounded to the nearest
+ * code, ties to even; infinities and NaN are stored as NaN. */
+int spk_kv8_append(void* stream, const uint16_t* qkv, const int32_t* slots, uint8_t* k8, uint8_t* v8, float* scales, int T,
+                   int blocks, int block_size, int Hq, int Hkv, int hd);
+
+/* o bf16 [B, Hq*hd]: row b = softmax(q_b K^T / sqrt(hd)) V over the first kv_len[b] positions of request b, which lie in the blocks
+ * of its row of table int32 [B, max_blocks]; q_b = the query part of row b of qkv bf16 [B, (Hq+2Hkv)*hd].  Positions in
+ * blocks outside the pool have weight 0, so have those behind max_blocks; a request without positions gives zeros.
+ * scratch: spk_kv8_attention_scratch_bytes bytes (may be NULL if that is 0); two calls that may overlap need
+ * one each.  B <= 65535. */
+size_t spk_kv8_attention_scratch_bytes(int B, int max_blocks, int block_size, int Hq, int Hkv, int hd);
+int spk_kv8_attention(void* stream, const uint16_t* qkv, const uint8_t* k8, const uint8_t* v8, const float* scales,
+                      const int32_t* table, const int32_t* kv_len, uint16_t* o, void* scratch, int B, int blocks,
+                      int block_size, int max_blocks, int Hq, int Hkv, int hd);
+/* How that call cuts the positions (host-only query): out2 (host) = {pieces of max_blocks * block_size, positions of a piece}. */
+int spk_kv8_plan(int B, int max_blocks, int block_size, int Hq, int Hkv, int* out2);
+
 #ifdef __cplusplus
 }
 #endif

@@ -142,6 +142,15 @@ _sig = {
     "spk_rmsnorm_bwd_static_max_d": (C.c_int, []),
     "spk_attention_bwd_scratch_bytes": (C.c_size_t, [C.c_int] * 5),
     "spk_attention_bwd": (C.c_int, [C.c_void_p] * 7 + [C.c_int] * 6),
+    "spk_batch_plan": (C.c_int, [C.c_void_p] * 4 + [C.c_int, C.c_void_p, C.c_int] + [C.c_void_p] * 3 + [C.c_int, C.c_void_p] +
+                       [C.c_int] * 2),
+    "spk_attention_packed": (C.c_int, [C.c_void_p] * 5 + [C.c_int] * 6),
+    "spk_attention_packed_bwd_scratch_bytes": (C.c_size_t, [C.c_int] * 2),
+    "spk_attention_packed_bwd": (C.c_int, [C.c_void_p] * 8 + [C.c_int] * 6),
+    "spk_kv8_append": (C.c_int, [C.c_void_p] * 6 + [C.c_int] * 6),
+    "spk_kv8_attention_scratch_bytes": (C.c_size_t, [C.c_int] * 6),
+    "spk_kv8_attention": (C.c_int, [C.c_void_p] * 9 + [C.c_int] * 7),
+    "spk_kv8_plan": (C.c_int, [C.c_int] * 5 + [_P(C.c_int)]),
 }
 for _n, (_r, _a) in _sig.items():
     _f = getattr(lib, _n)          # AttributeError here = header/library mismatch

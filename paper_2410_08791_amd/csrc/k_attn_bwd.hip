@@ -24,6 +24,7 @@
 // 2062 -> 1388; 8 x 1024, 16 heads of 128 399 -> 280; 4 x 1024, 64 query and 8 key heads of 128 748 -> 463;
 // 5 x 777, 32 and 8 heads of 64 231 -> 121; 32 x 257, 16 heads of 80, bidirectional 160 -> 145.
 #include "sp_gemm.h"
+#include "sp_packed.h"
 
 namespace {
 
@@ -116,10 +117,12 @@ __device__ __forceinline__ f32x16_t zero16() {
 // A work-group owns 128 queries of one head (a wave 32 of them, one query per lane as the B
 // operand) and walks 64-key tiles: S^T = K Q^T and dP^T = V dO^T read the tiles straight,
 // dQ^T += K^T dS^T reads K through the transposing LDS read.
-template <int HD>
+// PACKED: the sequences of sp_packed.h (S = rows of the buffers; lse and delta [Hq][S]), a slot per 128 rows.
+template <int HD, bool PACKED>
 __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dO,
                                                           const float* __restrict__ lse, const float* __restrict__ delta,
-                                                          bf16_t* __restrict__ dqkv, int S, int Hq, int Hkv, int ld_qkv,
+                                                          bf16_t* __restrict__ dqkv, const int* __restrict__ cu, int n_seqs,
+                                                          int S, int Hq, int Hkv, int ld_qkv,
                                                           int causal, float scale, float scale_log2e) {
     typedef TokTile<HD> T;
     typedef StageLoad<HD, 4> Load;
@@ -134,10 +137,18 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(const bf16_t* __res
     const int job = xcd_remap(blockIdx.x + (int)gridDim.x * (blockIdx.y + (int)gridDim.y * blockIdx.z),
                               (int)(gridDim.x * gridDim.y * gridDim.z));
     const int bx = job % (int)gridDim.x, h = (job / (int)gridDim.x) % (int)gridDim.y, b = job / (int)(gridDim.x * gridDim.y);
-    const int qb = causal ? gridDim.x - 1 - bx : bx;
+    int qb = causal ? gridDim.x - 1 - bx : bx;
+    size_t tok0 = (size_t)b * S, row0 = ((size_t)b * Hq + h) * S;       // row0: of lse and delta
+    if (PACKED) {
+        const PackedBlock p = packed_block<128>(cu, n_seqs, S, bx);
+        if (p.blk * 128 >= p.len) return;
+        qb = p.blk;
+        tok0 = p.row0;
+        row0 = (size_t)h * S + p.row0;
+        S = p.len;
+    }
     const int kvh = h / (Hq / Hkv);
     const int q0 = qb * 128, wq0 = q0 + wave * 32, qi = wq0 + l32;
-    const size_t tok0 = (size_t)b * S;
     const int qr = min(qi, S - 1);
     const bf16_t* kbase = qkv + tok0 * ld_qkv + (size_t)Hq * HD + (size_t)kvh * HD;
     const bf16_t* vbase = kbase + (size_t)Hkv * HD;
@@ -157,8 +168,8 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(const bf16_t* __res
             dof[ks] = *reinterpret_cast<const bf16x8_t*>(dp + ks * 16);
         }
     }
-    const float lse_q = lse[((size_t)b * Hq + h) * S + qr] * 1.4426950408889634f;
-    const float delta_q = delta[((size_t)b * Hq + h) * S + qr];
+    const float lse_q = lse[row0 + qr] * 1.4426950408889634f;
+    const float delta_q = delta[row0 + qr];
     int kpos[T::NKS], tpos[T::NMT];
 #pragma unroll
     for (int ks = 0; ks < T::NKS; ++ks) kpos[ks] = T::row_pos(ks, l32, half);
@@ -240,10 +251,11 @@ struct DkvCfg {
     static_assert(4 * TokTile<HD>::NMT * 16 * 256 <= 2 * StageLoad<HD, 8>::STAGE, "one accumulator set of four waves fits the stages");
 };
 
-template <int HD>
+template <int HD, bool PACKED>
 __global__ __launch_bounds__(512) void attn_bwd_dkv_kernel(const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dO,
                                                            const float* __restrict__ lse, const float* __restrict__ delta,
-                                                           bf16_t* __restrict__ dqkv, int S, int Hq, int Hkv,
+                                                           bf16_t* __restrict__ dqkv, const int* __restrict__ cu, int n_seqs,
+                                                           int S, int Hq, int Hkv,
                                                            int ld_qkv, int causal, float scale, float scale_log2e) {
     typedef TokTile<HD> T;
     typedef StageLoad<HD, 8> Load;
@@ -258,10 +270,19 @@ __global__ __launch_bounds__(512) void attn_bwd_dkv_kernel(const bf16_t* __restr
     // the same XCD-contiguous order as in the dq kernel: the key blocks of a head share its queries
     const int job = xcd_remap(blockIdx.x + (int)gridDim.x * (blockIdx.y + (int)gridDim.y * blockIdx.z),
                               (int)(gridDim.x * gridDim.y * gridDim.z));
-    const int bx = job % (int)gridDim.x, kvh = (job / (int)gridDim.x) % (int)gridDim.y, b = job / (int)(gridDim.x * gridDim.y);
+    int bx = job % (int)gridDim.x;
+    const int kvh = (job / (int)gridDim.x) % (int)gridDim.y, b = job / (int)(gridDim.x * gridDim.y);
     const int grp = Hq / Hkv;
+    size_t tok0 = (size_t)b * S, row0 = (size_t)b * Hq * S, ld_row = S;      // row0, ld_row: of lse and delta
+    if (PACKED) {
+        const PackedBlock p = packed_block<128>(cu, n_seqs, S, bx);
+        if (p.blk * 128 >= p.len) return;
+        // the first key block has the most queries under a causal mask
+        bx = causal ? (p.len - 1) / 128 - p.blk : p.blk;
+        tok0 = row0 = p.row0;
+        S = p.len;
+    }
     const int k0 = bx * 128, wk0 = k0 + kg * 32, kj = wk0 + l32;
-    const size_t tok0 = (size_t)b * S;
     const int ld_do = Hq * HD;
     const bf16_t* kbase = qkv + tok0 * ld_qkv + (size_t)Hq * HD + (size_t)kvh * HD;
     const bf16_t* vbase = kbase + (size_t)Hkv * HD;
@@ -278,7 +299,7 @@ __global__ __launch_bounds__(512) void attn_bwd_dkv_kernel(const bf16_t* __restr
         const int q0 = q_begin + (tile % tiles_per_head) * QT;
         ld.issue(smem + (tile & 1) * Load::STAGE, wave, qkv + tok0 * ld_qkv + h * HD, ld_qkv, dO + tok0 * ld_do + h * HD, ld_do, q0, S - 1, S - 1);
         if (threadIdx.x < QT) {
-            const size_t row = ((size_t)b * Hq + h) * S + min(q0 + (int)threadIdx.x, S - 1);
+            const size_t row = row0 + h * ld_row + min(q0 + (int)threadIdx.x, S - 1);
             r_lse = lse[row] * 1.4426950408889634f;
             r_delta = delta[row];
         }
@@ -393,22 +414,24 @@ __global__ __launch_bounds__(512) void attn_bwd_dkv_kernel(const bf16_t* __restr
     if (sub == 1) take_and_store(dv, Hkv, 1.0f);
 }
 
-template <int HD>
-hipError_t launch_bwd(hipStream_t st, const AttnBwdArgs& g, const AttnShape& a) {
+// B sequences of S rows, or (cu != nullptr) n_seqs packed ones in S rows.
+template <int HD, bool PACKED>
+hipError_t launch_bwd(hipStream_t st, const AttnBwdArgs& g, const AttnShape& a, const int* cu, int n_seqs) {
     constexpr int LDS_Q = 2 * StageLoad<HD, 4>::STAGE, LDS_KV = DkvCfg<HD>::LDS;
     static LdsLimitOnce lim_q, lim_kv;
-    hipError_t e = lim_q.set(reinterpret_cast<const void*>(attn_bwd_dq_kernel<HD>), LDS_Q);
-    if (e == hipSuccess) e = lim_kv.set(reinterpret_cast<const void*>(attn_bwd_dkv_kernel<HD>), LDS_KV);
+    hipError_t e = lim_q.set(reinterpret_cast<const void*>(attn_bwd_dq_kernel<HD, PACKED>), LDS_Q);
+    if (e == hipSuccess) e = lim_kv.set(reinterpret_cast<const void*>(attn_bwd_dkv_kernel<HD, PACKED>), LDS_KV);
     if (e != hipSuccess) return e;
     const float scale = 1.0f / sqrtf((float)a.hd), sl2 = scale * 1.4426950408889634f;
-    dim3 gq((a.S + 127) / 128, a.Hq, a.B);
-    attn_bwd_dq_kernel<HD><<<gq, 256, LDS_Q, st>>>(g.qkv, g.dO, g.lse, g.delta, g.dqkv, a.S, a.Hq, a.Hkv, a.ld_qkv, a.causal,
-                                                   scale, sl2);
+    const int blocks = PACKED ? a.S / 128 + n_seqs : (a.S + 127) / 128;
+    dim3 gq(blocks, a.Hq, a.B);
+    attn_bwd_dq_kernel<HD, PACKED><<<gq, 256, LDS_Q, st>>>(g.qkv, g.dO, g.lse, g.delta, g.dqkv, cu, n_seqs, a.S, a.Hq, a.Hkv, a.ld_qkv,
+                                                           a.causal, scale, sl2);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    dim3 gk((a.S + 127) / 128, a.Hkv, a.B);
-    attn_bwd_dkv_kernel<HD><<<gk, 512, LDS_KV, st>>>(g.qkv, g.dO, g.lse, g.delta, g.dqkv, a.S, a.Hq, a.Hkv, a.ld_qkv,
-                                                     a.causal, scale, sl2);
+    dim3 gk(blocks, a.Hkv, a.B);
+    attn_bwd_dkv_kernel<HD, PACKED><<<gk, 512, LDS_KV, st>>>(g.qkv, g.dO, g.lse, g.delta, g.dqkv, cu, n_seqs, a.S, a.Hq, a.Hkv, a.ld_qkv,
+                                                             a.causal, scale, sl2);
     return hipGetLastError();
 }
 
@@ -419,9 +442,19 @@ hipError_t spk_launch_attention_bwd(hipStream_t st, const AttnBwdArgs& g, const 
     if (a.Hkv <= 0 || a.Hq % a.Hkv || a.ld_qkv % 8 || a.B > 65535 || a.Hq > 65535) return hipErrorInvalidValue;
     if (!g.qkv || !g.dO || !g.lse || !g.delta || !g.dqkv) return hipErrorInvalidValue;
     switch (a.hd) {
-        case 64: return launch_bwd<64>(st, g, a);
-        case 80: return launch_bwd<80>(st, g, a);
-        case 128: return launch_bwd<128>(st, g, a);
+        case 64: return launch_bwd<64, false>(st, g, a, nullptr, 0);
+        case 80: return launch_bwd<80, false>(st, g, a, nullptr, 0);
+        case 128: return launch_bwd<128, false>(st, g, a, nullptr, 0);
+    }
+    return hipErrorInvalidValue;
+}
+
+hipError_t spk_launch_attention_packed_bwd(hipStream_t st, const AttnBwdArgs& g, const PackedShape& a) {
+    const AttnShape s{1, a.T, a.Hq, a.Hkv, a.hd, a.causal, (a.Hq + 2 * a.Hkv) * a.hd};
+    switch (a.hd) {
+        case 64: return launch_bwd<64, true>(st, g, s, a.cu, a.n);
+        case 80: return launch_bwd<80, true>(st, g, s, a.cu, a.n);
+        case 128: return launch_bwd<128, true>(st, g, s, a.cu, a.n);
     }
     return hipErrorInvalidValue;
 }

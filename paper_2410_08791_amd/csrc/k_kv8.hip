@@ -1,0 +1,409 @@
+// A block cache of keys and values in 8 bits: appending to it and single-query attention over it.
+//
+// One layer's cache is a pool of blocks of BS = 16, 32 or 64 tokens:
+//   k8 [blocks][Hkv][BS][hd]   e4m3, a token's head-dimension elements contiguous
+//   v8 [blocks][Hkv][hd][BS]   e4m3, an element's tokens contiguous
+//   scales fp32 [blocks][Hkv][2]   of a block's keys and values: what is stored is e4m3(x / scale).
+// A scale is 2^e, the smallest e >= -126 with max |x| <= 448 * 2^e (448 = the largest e4m3 value).  A power of two costs
+// nothing against max / 448 (e4m3 is a floating type: its relative step is the same at every magnitude) and buys
+// exactness: x / scale and code * scale are exact, so a stored value is off by the one rounding to e4m3 (half a step,
+// 2^-4 relative, 2^-10 scale below 2^-6 scale), and a block whose scale grows while it fills is re-coded by an exact
+// shift of the exponent (a second rounding only where a code falls below the normal range).
+#include "sp_attn.h"
+#include "sp_kernels.h"
+
+namespace {
+
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ float exp2_bits(int biased) { return __uint_as_float((uint32_t)biased << 23); }
+
+// ---------------------------------------------------------------------------------------------- append
+// A run is a maximal row of tokens with consecutive slots inside one block.  One wave writes the keys, another the values
+// of one block and head, run after run in the order of the rows, and nobody else touches them: a row whose block
+// occurs in the 64 rows before it leaves the block to the wave that met it first.  The wave holds the whole run in registers (64 tokens of 128: 64
+// VGPRs), so it is read once, between the largest value and the coding.  Lane (rg, c) has the block positions
+// rg * TPL .. rg * TPL + TPL - 1 of the elements 8 c .. 8 c + 7: a row of keys leaves in pieces of 8 bytes, and the
+// transposition that the value layout needs happens inside the lane.
+// HBM-bound for prompts (4 bytes read and 2 written per token, head and element), latency-bound for single tokens: their
+// block is read again only where its scale grows.
+// What a run needs to know comes from the slots alone: `range` tokens per wave are looked at for the beginning of a run.
+template <int HD, int BS>
+__global__ __launch_bounds__(256) void kv8_append_kernel(const bf16_t* __restrict__ qkv, const int* __restrict__ slots, int T, int range,
+                                                         int Hq, Kv8Cache c) {
+    constexpr int LPR = HD / 8, RPI = 64 / LPR, TPL = BS / RPI;      // lanes per row, rows per instruction, positions per lane
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rg = lane / LPR, ch = lane % LPR;
+    const int Hkv = c.Hkv, ld = (Hq + 2 * Hkv) * HD;
+    const int isv = blockIdx.y & 1, h = blockIdx.y >> 1;
+    const int limit = c.blocks * BS;
+    const int begin = ((int)blockIdx.x * 4 + wave) * range;         // T <= 2^30
+    if (begin >= T) return;
+    auto slot_at = [&](int row) { return row >= 0 && row < T ? slots[row] : -1; };
+    const int before = slot_at(begin - 64 + lane), from = slot_at(begin + lane);
+    for (int i = 0; i < range && begin + i < T; ++i) {
+        int t = begin + i;
+        int s = __builtin_amdgcn_readfirstlane(__shfl(from, i, 64));
+        if (s < 0 || s >= limit) continue;
+        const int block = s / BS;
+        auto here = [&](int slot) { return slot >= 0 && slot / BS == block; };
+        if (__any(lane >= i ? here(before) : here(from))) continue;      // one of the 64 rows in front of t
+        for (;;) {
+        const int off = s % BS;
+        // the run's length: its slots follow one another up to the end of the block
+        const bool in = lane < BS - off && slot_at(t + lane) == s + lane;
+        const unsigned long long miss = ~__ballot(in);
+        const int m = miss ? __builtin_ctzll(miss) : 64;
+        const size_t bh = (size_t)block * Hkv + h;
+        const bf16_t* src = qkv + (size_t)t * ld + (size_t)(Hq + isv * Hkv + h) * HD + ch * 8;
+        u32x4_t x[TPL];
+        uint32_t big = 0;
+#pragma unroll
+        for (int i = 0; i < TPL; ++i) {
+            const int p = rg * TPL + i - off;                        // token of the run
+            x[i] = u32x4_t{0, 0, 0, 0};
+            if (p >= 0 && p < m) x[i] = *reinterpret_cast<const u32x4_t*>(src + (size_t)p * ld);
+        }
+#pragma unroll
+        for (int i = 0; i < TPL; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const u16x2_t a = __builtin_bit_cast(u16x2_t, x[i][k] & 0x7fff7fffu);
+                big = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, big), a));
+            }
+        int top = max(big & 0xffff, big >> 16);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o, 64));
+        const bool odd = top >= 0x7f80;                              // infinities or NaN among them: stored as NaN, the scale is the others'
+        if (odd) {
+            top = 0;
+#pragma unroll
+            for (int i = 0; i < TPL; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int lo = x[i][k] & 0x7fff, hi = (x[i][k] >> 16) & 0x7fff;
+                    top = max(top, max(lo < 0x7f80 ? lo : 0, hi < 0x7f80 ? hi : 0));
+                }
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o, 64));
+        }
+        // biased exponent of the scale: 1.75 * 2^8 is the largest code
+        int e = max((top >> 7) - 8 + ((top & 127) > 96 ? 1 : 0), 1);
+        float* sp = c.scales + bh * 2 + isv;
+        const int e_old = off ? min(max((int)((__float_as_uint(*sp) >> 23) & 255), 1), 253) : 0;
+        e = max(e, e_old);
+        const bool grow = off && e > e_old;
+        const float inv = exp2_bits(254 - e), shift = exp2_bits(max(127 + e_old - e, 0));
+        if (lane == 0 && e != e_old) *sp = exp2_bits(e);
+        auto code4 = [&](uint32_t w0, uint32_t w1) {                 // four bf16 values
+            int r = __builtin_amdgcn_cvt_pk_fp8_f32(bf_lo(w0) * inv, bf_hi(w0) * inv, 0, false);
+            r = __builtin_amdgcn_cvt_pk_fp8_f32(bf_lo(w1) * inv, bf_hi(w1) * inv, r, true);
+            if (odd) {
+                const uint32_t w[2] = {w0, w1};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t v = w[k >> 1] >> (16 * (k & 1));
+                    if ((v & 0x7fff) >= 0x7f80) r = (r & ~(255u << (8 * k))) | ((127u | (v >> 8 & 128u)) << (8 * k));
+                }
+            }
+            return (uint32_t)r;
+        };
+        auto recode4 = [&](uint32_t w) {
+            const f32x2_t a = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+            int r = __builtin_amdgcn_cvt_pk_fp8_f32(a.x * shift, a.y * shift, 0, false);
+            return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(b.x * shift, b.y * shift, r, true);
+        };
+        if (!isv) {
+            uint8_t* dst = c.k8 + bh * (BS * HD) + ch * 8;
+#pragma unroll
+            for (int i = 0; i < TPL; ++i) {
+                const int p = rg * TPL + i;
+                uint32_t* d = reinterpret_cast<uint32_t*>(dst + p * HD);
+                if (p >= off && p < off + m) {
+                    *reinterpret_cast<uint2*>(d) = make_uint2(code4(x[i][0], x[i][1]), code4(x[i][2], x[i][3]));
+                } else if (grow && p < off) {
+                    const uint2 o = *reinterpret_cast<const uint2*>(d);
+                    *reinterpret_cast<uint2*>(d) = make_uint2(recode4(o.x), recode4(o.y));
+                }
+            }
+        } else {
+            uint8_t* dst = c.v8 + bh * (BS * HD) + (size_t)ch * 8 * BS + rg * TPL;
+            uint32_t y[TPL][2];
+#pragma unroll
+            for (int i = 0; i < TPL; ++i) { y[i][0] = code4(x[i][0], x[i][1]); y[i][1] = code4(x[i][2], x[i][3]); }
+            const int p0 = rg * TPL;
+            const bool whole = p0 >= off && p0 + TPL <= off + m;
+            const bool some = p0 < off + m && p0 + TPL > (grow ? 0 : off);
+            if (whole) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    uint32_t w[(TPL + 3) / 4] = {};
+#pragma unroll
+                    for (int i = 0; i < TPL; ++i) w[i / 4] |= ((y[i][k >> 2] >> (8 * (k & 3))) & 255u) << (8 * (i & 3));
+                    if constexpr (TPL == 16) *reinterpret_cast<u32x4_t*>(dst + k * BS) = u32x4_t{w[0], w[1], w[2], w[3]};
+                    else if constexpr (TPL == 8) *reinterpret_cast<uint2*>(dst + k * BS) = make_uint2(w[0], w[1]);
+                    else if constexpr (TPL == 4) *reinterpret_cast<uint32_t*>(dst + k * BS) = w[0];
+                    else *reinterpret_cast<uint16_t*>(dst + k * BS) = (uint16_t)w[0];
+                }
+            } else if (some) {
+#pragma unroll
+                for (int i = 0; i < TPL; ++i) {
+                    const int p = p0 + i;
+                    if (p >= off && p < off + m) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) dst[k * BS + i] = (uint8_t)(y[i][k >> 2] >> (8 * (k & 3)));
+                    } else if (grow && p < off) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) dst[k * BS + i] = (uint8_t)recode4(dst[k * BS + i]);
+                    }
+                }
+            }
+        }
+        // the block's next run, if the rows that follow have one; it reads what this one wrote
+        const unsigned long long more = __ballot(here(slot_at(t + m + lane)));
+        if (!more) break;
+        t += m + __builtin_ctzll(more);
+        s = slots[t];
+        __threadfence_block();
+        }
+    }
+}
+
+template <int HD>
+hipError_t launch_append(hipStream_t st, const bf16_t* qkv, const int* slots, int T, int Hq, const Kv8Cache& c) {
+    const int range = (long)T * c.Hkv * 2 <= 16384 ? 1 : 4;
+    const dim3 grid((unsigned)(((long)T + 4 * range - 1) / (4 * range)), c.Hkv * 2);
+    switch (c.block_size) {
+        case 16: kv8_append_kernel<HD, 16><<<grid, 256, 0, st>>>(qkv, slots, T, range, Hq, c); break;
+        case 32: kv8_append_kernel<HD, 32><<<grid, 256, 0, st>>>(qkv, slots, T, range, Hq, c); break;
+        case 64: kv8_append_kernel<HD, 64><<<grid, 256, 0, st>>>(qkv, slots, T, range, Hq, c); break;
+        default: return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+}
+
+// ------------------------------------------------------------------------------------------- attention
+// o = softmax(q K^T / sqrt(hd)) V for one query per request over its first kv_len positions.
+//
+// HBM-bound: 2 Hkv hd bytes per position.  A wave walks 64 positions at a time on its own, 16 loads of 16 bytes per lane
+// in flight at hd 128.  Both products are v_mfma_f32_16x16x32_bf16 on codes converted to bf16 (exact), the query heads
+// that share a key/value head being the 16 columns: S^T = K Q^T, then O^T = V^T P^T.  In the accumulators of S^T a lane
+// (column r = head, row group g) holds four rows of a 16-row tile; the rows of the four tiles are assigned to positions so
+// that these are the positions 16 g .. 16 g + 15, in the order in which the lane's bytes of a V row come: P^T in bf16 is
+// then the B operand as it stands, K and V are read as they lie, and all that a lane weighs belongs to one block -- one
+// key scale, which multiplies its scores, and one value scale, which the conversion applies.
+constexpr int NW8 = 4;
+
+__device__ __forceinline__ bf16x8_t bf16_of_codes(uint32_t a, uint32_t b, float scale) {
+    union { bf16x2_t p[4]; bf16x8_t v; } u;
+    u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false);
+    u.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true);
+    u.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false);
+    u.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
+    return u.v;
+}
+
+template <int HD>
+__global__ __launch_bounds__(NW8 * 64) void kv8_attn_kernel(const bf16_t* __restrict__ qkv, Kv8Cache c, const int* __restrict__ table,
+                                                            const int* __restrict__ kv_len, bf16_t* __restrict__ o,
+                                                            float* __restrict__ part, int lbs, int max_blocks, int Hq, int splits,
+                                                            int per, float scale_log2e) {
+    constexpr int NJ = HD / 64, NT = HD / 16;
+    __shared__ __attribute__((aligned(16))) float buf[NW8][16][HD + 4];
+    __shared__ float wm[NW8][16], wl[NW8][16];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, g = lane >> 4;
+    const int Hkv = c.Hkv, grp = Hq / Hkv, ngb = (grp + 15) / 16;
+    const int split = blockIdx.x, hk = blockIdx.y / ngb, h0 = (blockIdx.y % ngb) * 16, b = blockIdx.z;
+    const int bs = 1 << lbs;
+    const int n = min(max(kv_len[b], 0), max_blocks << lbs);
+    const int s0 = split * per, s1 = min(n, s0 + per);
+    if (splits > 1 && s0 >= n && split > 0) return;      // the combination reads ceil(n / per) pieces, at least one
+    const int heads = min(grp - h0, 16);
+    const int hq = hk * grp + h0;
+
+    bf16x8_t qf[NJ][2];
+    {
+        const bf16_t* qp = qkv + (size_t)b * ((Hq + 2 * Hkv) * HD) + (size_t)(hq + min(r, heads - 1)) * HD + g * 16;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) qf[j][s] = *reinterpret_cast<const bf16x8_t*>(qp + j * 64 + s * 8);
+    }
+    const int* row = table + (size_t)b * max_blocks;
+    f32x4_t acc[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float m_run = -3.402823466e38f, l_run = 0.f;
+    for (int t0 = s0 + w * 64; t0 < s1; t0 += NW8 * 64) {
+        // the block that holds the positions t0 + 16 x .. of a group x of 16; nothing where there are none or the entry is no block
+        auto block_of = [&](int x, bool* ok) {
+            const int t = t0 + 16 * x;
+            const int k = row[min(t, n - 1) >> lbs];
+            *ok = t < n && (unsigned)k < (unsigned)c.blocks;
+            return (size_t)(*ok ? k : 0) * Hkv + hk;
+        };
+        bool ok_k, ok_v;
+        const size_t bk = block_of(r >> 2, &ok_k), bv = block_of(g, &ok_v);
+        const uint8_t* kp = c.k8 + (bk << lbs) * HD + (((t0 + 16 * (r >> 2)) & (bs - 1)) + (r & 3)) * HD + g * 16;
+        const uint8_t* vp = c.v8 + (bv << lbs) * HD + (r << lbs) + ((t0 + 16 * g) & (bs - 1));
+        const float2 sc = *reinterpret_cast<const float2*>(c.scales + bv * 2);
+        u32x4_t kw[4][NJ], vw[NT];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) kw[t][j] = *reinterpret_cast<const u32x4_t*>(kp + t * 4 * HD + j * 64);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) vw[t] = *reinterpret_cast<const u32x4_t*>(vp + ((t * 16) << lbs));
+        f32x4_t s[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of_codes(kw[t][j][0], kw[t][j][1], 1.0f), qf[j][0], s[t], 0, 0, 0);
+                s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of_codes(kw[t][j][2], kw[t][j][3], 1.0f), qf[j][1], s[t], 0, 0, 0);
+            }
+        }
+        const int left = ok_v ? min(max(n - (t0 + 16 * g), 0), 16) : 0;      // positions of this lane's 16
+        const float sk = sc.x * scale_log2e;
+        float mx = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[t][i] = t * 4 + i < left ? s[t][i] * sk : -INFINITY;
+                mx = fmaxf(mx, s[t][i]);
+            }
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const float m_new = fmaxf(m_run, mx);
+        const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+        m_run = m_new;
+        bf16x8_t pf[2];
+        float sum = 0.f;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float p = __builtin_amdgcn_exp2f(s[t][i] - m_new);
+                sum += p;
+                pf[t >> 1][(t & 1) * 4 + i] = (__bf16)p;
+            }
+        l_run = fmaf(l_run, alpha, sum);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[t] *= alpha;
+        if (__any(left < 16)) {
+            // what lies behind the last position is whatever the block held before, NaN codes included
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int live = min(max(left - 4 * k, 0), 4);
+                    vw[t][k] &= live == 4 ? 0xffffffffu : (1u << (8 * live)) - 1;
+                }
+        }
+        const float sv = left ? sc.y : 1.0f;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of_codes(vw[t][0], vw[t][1], sv), pf[0], acc[t], 0, 0, 0);
+            acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of_codes(vw[t][2], vw[t][3], sv), pf[1], acc[t], 0, 0, 0);
+        }
+    }
+    l_run += __shfl_xor(l_run, 16, 64);
+    l_run += __shfl_xor(l_run, 32, 64);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4_t*>(&buf[w][r][t * 16 + 4 * g]) = acc[t];
+    if (g == 0) { wm[w][r] = m_run; wl[w][r] = l_run; }
+    __syncthreads();
+    for (int i = threadIdx.x; i < heads * HD; i += NW8 * 64) {
+        const int head = i / HD, d = i % HD;
+        float M = wm[0][head];
+#pragma unroll
+        for (int k = 1; k < NW8; ++k) M = fmaxf(M, wm[k][head]);
+        float L = 0.f, a = 0.f;
+#pragma unroll
+        for (int k = 0; k < NW8; ++k) {
+            const float f = __builtin_amdgcn_exp2f(wm[k][head] - M);
+            L = fmaf(f, wl[k][head], L);
+            a = fmaf(f, buf[k][head][d], a);
+        }
+        if (splits == 1) {
+            o[((size_t)b * Hq + hq + head) * HD + d] = f2bf(L == 0.f ? 0.f : a / L);
+        } else {
+            float* pr = part + (((size_t)b * Hq + hq + head) * splits + split) * (HD + 2);
+            pr[d] = a;
+            if (d == 0) { pr[HD] = M; pr[HD + 1] = L; }
+        }
+    }
+}
+
+// o from the pieces of a request's positions, in their order.
+template <int HD>
+__global__ __launch_bounds__(HD) void kv8_combine_kernel(const float* __restrict__ part, const int* __restrict__ kv_len,
+                                                         bf16_t* __restrict__ o, int splits, int per, int most, int Hq) {
+    const int hq = blockIdx.x, b = blockIdx.y, d = threadIdx.x;
+    const int pieces = max((min(max(kv_len[b], 0), most) + per - 1) / per, 1);
+    const float* p = part + ((size_t)b * Hq + hq) * splits * (HD + 2);
+    float M = -INFINITY, L = 0.f, a = 0.f;
+    for (int s = 0; s < pieces; ++s) M = fmaxf(M, p[s * (HD + 2) + HD]);
+    for (int s = 0; s < pieces; ++s) {
+        const float f = __builtin_amdgcn_exp2f(p[s * (HD + 2) + HD] - M);
+        L = fmaf(f, p[s * (HD + 2) + HD + 1], L);
+        a = fmaf(f, p[s * (HD + 2) + d], a);
+    }
+    o[((size_t)b * Hq + hq) * HD + d] = f2bf(L == 0.f ? 0.f : a / L);
+}
+
+struct Kv8Plan { int splits, per; };
+
+Kv8Plan plan_kv8(int B, int max_blocks, int block_size, int Hq, int Hkv) {
+    const long most = (long)max_blocks * block_size;
+    const int grp = Hq / Hkv;
+    const long groups = (long)B * Hkv * ((grp + 15) / 16);
+    const long splits = std::max(std::min((2048 + groups - 1) / groups, (most + 511) / 512), 1L);
+    Kv8Plan p;
+    p.per = (int)(((most + splits - 1) / splits + 255) / 256 * 256);
+    p.splits = (int)((most + p.per - 1) / p.per);
+    return p;
+}
+
+template <int HD>
+hipError_t launch_kv8(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* part, const int* table, const int* kv_len, int B,
+                      int max_blocks, int Hq, const Kv8Cache& c) {
+    const Kv8Plan p = plan_kv8(B, max_blocks, c.block_size, Hq, c.Hkv);
+    const int lbs = c.block_size == 16 ? 4 : c.block_size == 32 ? 5 : 6, grp = Hq / c.Hkv;
+    if (p.splits > 1 && !part) return hipErrorInvalidValue;
+    kv8_attn_kernel<HD><<<dim3(p.splits, c.Hkv * ((grp + 15) / 16), B), NW8 * 64, 0, st>>>(
+        qkv, c, table, kv_len, o, part, lbs, max_blocks, Hq, p.splits, p.per, 1.4426950408889634f / sqrtf((float)HD));
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.splits == 1) return e;
+    kv8_combine_kernel<HD><<<dim3(Hq, B), HD, 0, st>>>(part, kv_len, o, p.splits, p.per, max_blocks << lbs, Hq);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t spk_launch_kv8_append(hipStream_t st, const bf16_t* qkv, const int* slots, int T, int Hq, const Kv8Cache& c) {
+    return c.hd == 128 ? launch_append<128>(st, qkv, slots, T, Hq, c) : c.hd == 64 ? launch_append<64>(st, qkv, slots, T, Hq, c)
+                                                                                : hipErrorInvalidValue;
+}
+
+void spk_kv8_plan_host(int B, int max_blocks, int block_size, int Hq, int Hkv, int* out2) {
+    const Kv8Plan p = plan_kv8(B, max_blocks, block_size, Hq, Hkv);
+    out2[0] = p.splits; out2[1] = p.per;
+}
+
+size_t spk_kv8_scratch_bytes(int B, int max_blocks, int block_size, int Hq, int Hkv, int hd) {
+    const Kv8Plan p = plan_kv8(B, max_blocks, block_size, Hq, Hkv);
+    return p.splits == 1 ? 0 : (size_t)B * Hq * p.splits * (hd + 2) * 4;
+}
+
+hipError_t spk_launch_kv8_attention(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* part, const int* table, const int* kv_len, int B,
+                                    int max_blocks, int Hq, const Kv8Cache& c) {
+    return c.hd == 128  ? launch_kv8<128>(st, qkv, o, part, table, kv_len, B, max_blocks, Hq, c)
+           : c.hd == 64 ? launch_kv8<64>(st, qkv, o, part, table, kv_len, B, max_blocks, Hq, c)
+                        : hipErrorInvalidValue;
+}

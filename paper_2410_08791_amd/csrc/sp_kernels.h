@@ -142,3 +142,40 @@ struct AttnBwdArgs {
     bf16_t* dqkv;
 };
 hipError_t spk_launch_attention_bwd(hipStream_t st, const AttnBwdArgs& g, const AttnShape& a);
+
+// ---- packed batches: requests of different lengths ------------------------------------------
+// Their rows lie one behind the other: sequence r has the rows cu[r] .. cu[r + 1] - 1 of T.  The device-side lengths are
+// clamped to [0, T]; rows that belong to no sequence are neither read nor written (the row sums of the backward pass aside,
+// which go into the scratch).  The callers below check n, T and the heads; see include/superpipe_kernels.h.
+struct PackedShape {
+    const int* cu;       // dev, n + 1
+    int n, T, Hq, Hkv, hd, causal;
+};
+// lse (nullable) fp32 [Hq, T].
+hipError_t spk_launch_attention_packed(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* lse, const PackedShape& a);
+// g.lse and g.delta fp32 [Hq, T].
+hipError_t spk_launch_attention_packed_bwd(hipStream_t st, const AttnBwdArgs& g, const PackedShape& a);
+
+struct BatchPlanArgs {
+    const int *lens, *cached, *free_blocks;   // cached: nullptr = nothing yet
+    int n_free;
+    int* table; int max_blocks;               // [n, max_blocks]
+    int *cu, *kv_len, *slots; int max_tokens;
+    int* info;
+    int n, block_size;
+};
+hipError_t spk_launch_batch_plan(hipStream_t st, const BatchPlanArgs& g);
+
+// One layer's block cache in 8 bits: k8 [blocks][Hkv][block_size][hd], v8 [blocks][Hkv][hd][block_size], e4m3;
+// scales fp32 [blocks][Hkv][2] (keys, values), powers of two.
+struct Kv8Cache {
+    uint8_t *k8, *v8;
+    float* scales;
+    int blocks, block_size, Hkv, hd;
+};
+hipError_t spk_launch_kv8_append(hipStream_t st, const bf16_t* qkv, const int* slots, int T, int Hq, const Kv8Cache& c);
+// Host: pieces that the positions of a request are cut into, and positions of a piece.
+void spk_kv8_plan_host(int B, int max_blocks, int block_size, int Hq, int Hkv, int* out2);
+size_t spk_kv8_scratch_bytes(int B, int max_blocks, int block_size, int Hq, int Hkv, int hd);
+hipError_t spk_launch_kv8_attention(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* part, const int* table, const int* kv_len, int B,
+                                    int max_blocks, int Hq, const Kv8Cache& c);

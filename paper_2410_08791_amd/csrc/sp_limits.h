@@ -9,6 +9,8 @@ constexpr int kDecodeMaxLen = 32768;      // longest key/value cache
 // Decode attention splits the positions while (sequences x key/value heads x splits) stays within this
 // many work-groups, two per CU; each leaves one row of partial results per query head.
 constexpr int kDecodeSplitGroups = 512;
+// Packed batches: most sequences of a call (their table is searched in two steps of a wave's 64 lanes).
+constexpr int kPackedMaxSeqs = 4096;
 inline size_t decode_scratch_floats(int n_q_heads, int n_kv_heads, int head_dim) {
     return (size_t)(n_q_heads / n_kv_heads) * kDecodeSplitGroups * (head_dim + 2);
 }

@@ -1,0 +1,115 @@
+// C ABI of the operators over packed batches: argument checks in front of the launchers.
+#include <limits.h>
+
+#include <initializer_list>
+
+#include "../../include/superpipe.h"
+#include "../../include/superpipe_kernels.h"
+#include "sp_kernels.h"
+
+static int st(hipError_t e) {
+    if (e == hipSuccess) return SP_OK;
+    (void)hipGetLastError();
+    return e == hipErrorInvalidValue ? SP_ERR_INVALID_ARG : SP_ERR_HIP;
+}
+
+static bool misaligned(int to, std::initializer_list<const void*> ptrs) {
+    uintptr_t all = 0;
+    for (const void* p : ptrs) all |= (uintptr_t)p;
+    return (all & (uintptr_t)(to - 1)) != 0;
+}
+
+static bool any_null(std::initializer_list<const void*> ptrs) {
+    for (const void* p : ptrs)
+        if (!p) return true;
+    return false;
+}
+
+constexpr int kMostPositions = 1 << 30;      // of a request, and rows of a packed batch: sums of a few of them fit an int
+
+static bool block_size_ok(int bs) { return bs == 16 || bs == 32 || bs == 64; }
+
+extern "C" int spk_batch_plan(void* stream, const int32_t* lens, const int32_t* cached, const int32_t* free_blocks, int n_free,
+                              int32_t* table, int max_blocks, int32_t* cu, int32_t* kv_len, int32_t* slots, int max_tokens,
+                              int32_t* info, int n, int block_size) {
+    if (any_null({lens, table, cu, kv_len, slots, info}) || (!free_blocks && n_free > 0)) return SP_ERR_INVALID_ARG;
+    if (misaligned(4, {lens, cached, free_blocks, table, cu, kv_len, slots, info}) || kv_len == cached) return SP_ERR_INVALID_ARG;
+    if (n < 1 || n > kPackedMaxSeqs || n_free < 0 || max_tokens < 1 || max_tokens > kMostPositions || !block_size_ok(block_size) ||
+        max_blocks < 1 || max_blocks > kMostPositions / block_size)
+        return SP_ERR_INVALID_ARG;
+    return st(spk_launch_batch_plan((hipStream_t)stream, BatchPlanArgs{lens, cached, free_blocks, n_free, table, max_blocks, cu, kv_len, slots,
+                                                                      max_tokens, info, n, block_size}));
+}
+
+// Everything but the pointers; slots of 32 rows are the most that any form launches per head.
+static bool packed_ok(int n, int T, int Hq, int Hkv, int hd) {
+    return n >= 1 && n <= kPackedMaxSeqs && T >= 1 && T <= kMostPositions && Hkv >= 1 && Hq >= Hkv && Hq % Hkv == 0 && Hq <= 65535 &&
+           (hd == 64 || hd == 80 || hd == 128) && ((long)T / 32 + n) * Hq <= INT_MAX / 512;
+}
+
+extern "C" int spk_attention_packed(void* stream, const uint16_t* qkv, const int32_t* cu, uint16_t* o, float* lse, int n, int T,
+                                    int Hq, int Hkv, int hd, int causal) {
+    if (any_null({qkv, cu, o}) || misaligned(16, {qkv, o}) || misaligned(4, {cu, lse}) || !packed_ok(n, T, Hq, Hkv, hd))
+        return SP_ERR_INVALID_ARG;
+    return st(spk_launch_attention_packed((hipStream_t)stream, qkv, o, lse, PackedShape{cu, n, T, Hq, Hkv, hd, causal != 0}));
+}
+
+extern "C" size_t spk_attention_packed_bwd_scratch_bytes(int T, int Hq) {
+    if (T < 1 || T > kMostPositions || Hq < 1) return 0;
+    return ((size_t)T * Hq * 4 + 255) / 256 * 256;     // delta = rowsum(dO * O)
+}
+
+extern "C" int spk_attention_packed_bwd(void* stream, const uint16_t* qkv, const int32_t* cu, const uint16_t* o, const uint16_t* dO,
+                                        const float* lse, void* scratch, uint16_t* dqkv, int n, int T, int Hq, int Hkv, int hd,
+                                        int causal) {
+    if (any_null({qkv, cu, o, dO, lse, scratch, dqkv}) || misaligned(16, {qkv, o, dO, scratch, dqkv}) || misaligned(4, {cu, lse}) ||
+        !packed_ok(n, T, Hq, Hkv, hd))
+        return SP_ERR_INVALID_ARG;
+    hipStream_t s = (hipStream_t)stream;
+    float* delta = static_cast<float*>(scratch);
+    hipError_t e = spk_launch_attn_delta(s, dO, o, delta, 1, T, Hq, hd);
+    if (e != hipSuccess) return st(e);
+    AttnBwdArgs g{qkv, dO, lse, delta, dqkv};
+    return st(spk_launch_attention_packed_bwd(s, g, PackedShape{cu, n, T, Hq, Hkv, hd, causal != 0}));
+}
+
+static bool cache_ok(int blocks, int block_size, int Hq, int Hkv, int hd) {
+    return block_size_ok(block_size) && blocks >= 1 && blocks <= INT_MAX / block_size && Hkv >= 1 && Hq >= Hkv && Hq % Hkv == 0 &&
+           Hq <= 32767 && (hd == 64 || hd == 128);
+}
+
+extern "C" int spk_kv8_append(void* stream, const uint16_t* qkv, const int32_t* slots, uint8_t* k8, uint8_t* v8, float* scales, int T,
+                              int blocks, int block_size, int Hq, int Hkv, int hd) {
+    if (any_null({qkv, slots, k8, v8, scales}) || misaligned(16, {qkv, k8, v8}) || misaligned(8, {scales}) || misaligned(4, {slots}))
+        return SP_ERR_INVALID_ARG;
+    if (T < 1 || T > kMostPositions || !cache_ok(blocks, block_size, Hq, Hkv, hd)) return SP_ERR_INVALID_ARG;
+    return st(spk_launch_kv8_append((hipStream_t)stream, qkv, slots, T, Hq, Kv8Cache{k8, v8, scales, blocks, block_size, Hkv, hd}));
+}
+
+static bool kv8_call_ok(int B, int max_blocks, int block_size, int Hq, int Hkv, int hd) {
+    return B >= 1 && B <= 65535 && cache_ok(1, block_size, Hq, Hkv, hd) && max_blocks >= 1 && max_blocks <= kMostPositions / block_size;
+}
+
+extern "C" int spk_kv8_plan(int B, int max_blocks, int block_size, int Hq, int Hkv, int* out2) {
+    if (!out2 || !kv8_call_ok(B, max_blocks, block_size, Hq, Hkv, 128)) return SP_ERR_INVALID_ARG;
+    spk_kv8_plan_host(B, max_blocks, block_size, Hq, Hkv, out2);
+    return SP_OK;
+}
+
+extern "C" size_t spk_kv8_attention_scratch_bytes(int B, int max_blocks, int block_size, int Hq, int Hkv, int hd) {
+    if (!kv8_call_ok(B, max_blocks, block_size, Hq, Hkv, hd)) return 0;
+    return spk_kv8_scratch_bytes(B, max_blocks, block_size, Hq, Hkv, hd);
+}
+
+extern "C" int spk_kv8_attention(void* stream, const uint16_t* qkv, const uint8_t* k8, const uint8_t* v8, const float* scales,
+                                 const int32_t* table, const int32_t* kv_len, uint16_t* o, void* scratch, int B, int blocks,
+                                 int block_size, int max_blocks, int Hq, int Hkv, int hd) {
+    if (any_null({qkv, k8, v8, scales, table, kv_len, o}) || misaligned(16, {qkv, k8, v8, o, scratch}) || misaligned(8, {scales}) ||
+        misaligned(4, {table, kv_len}))
+        return SP_ERR_INVALID_ARG;
+    if (!kv8_call_ok(B, max_blocks, block_size, Hq, Hkv, hd) || !cache_ok(blocks, block_size, Hq, Hkv, hd)) return SP_ERR_INVALID_ARG;
+    if (!scratch && spk_kv8_scratch_bytes(B, max_blocks, block_size, Hq, Hkv, hd)) return SP_ERR_INVALID_ARG;
+    return st(spk_launch_kv8_attention((hipStream_t)stream, qkv, o, static_cast<float*>(scratch), table, kv_len, B, max_blocks, Hq,
+                                       Kv8Cache{const_cast<uint8_t*>(k8), const_cast<uint8_t*>(v8), const_cast<float*>(scales), blocks,
+                                                block_size, Hkv, hd}));
+}
