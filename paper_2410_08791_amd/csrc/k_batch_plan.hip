@@ -13,7 +13,7 @@ namespace {
 
 constexpr int PLAN_THREADS = 512;
 constexpr int PER_THREAD = kPackedMaxSeqs / PLAN_THREADS;
-constexpr int TOKENS_PER_GROUP = 2048;
+constexpr int TOKENS_PER_GROUP = PLAN_THREADS;
 
 __device__ __forceinline__ long wave_scan(long v) {       // inclusive
     const int lane = threadIdx.x & 63;
@@ -30,8 +30,8 @@ __global__ __launch_bounds__(PLAN_THREADS) void batch_plan_kernel(BatchPlanArgs 
     __shared__ long w_tok[PLAN_THREADS / 64], w_new[PLAN_THREADS / 64];
     __shared__ int w_max[PLAN_THREADS / 64], w_bad[PLAN_THREADS / 64];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const int bs = g.block_size, n = g.n;
-    const long row = (long)g.max_blocks * bs;
+    const int lbs = __builtin_ctz(g.block_size), bs = 1 << lbs, n = g.n;
+    const long row = (long)g.max_blocks << lbs;
     // consecutive requests per thread
     long tok = 0, fresh = 0;
     int longest = 0, bad = 0;
@@ -45,7 +45,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void batch_plan_kernel(BatchPlanArgs 
             const int L = g.lens[r], c = g.cached ? g.cached[r] : 0;
             bad |= (L < 0 || c < 0) ? 8 : (long)L + c > row ? 4 : 0;
             len[i] = max(L, 0);
-            need[i] = (int)(((long)max(c, 0) + len[i] + bs - 1) / bs - ((long)max(c, 0) + bs - 1) / bs);
+            need[i] = (int)((((long)max(c, 0) + len[i] + bs - 1) >> lbs) - (((long)max(c, 0) + bs - 1) >> lbs));
             longest = max(longest, len[i]);
         }
         tok += len[i];
@@ -110,15 +110,15 @@ __global__ __launch_bounds__(PLAN_THREADS) void batch_plan_kernel(BatchPlanArgs 
     const int all_new = s_new[n];
     for (int i = first; i < all_new; i += step) {
         const int r = owner(s_new, i), c = g.cached ? g.cached[r] : 0;
-        g.table[(size_t)r * g.max_blocks + (c + bs - 1) / bs + i - s_new[r]] = g.free_blocks[i];
+        g.table[(size_t)r * g.max_blocks + ((c + bs - 1) >> lbs) + i - s_new[r]] = g.free_blocks[i];
     }
     for (int t = first; t < g.max_tokens; t += step) {
         int slot = -1;
         if (t < tokens) {
             const int r = owner(s_tok, t), c = g.cached ? g.cached[r] : 0;
-            const int pos = c + t - s_tok[r], held = (c + bs - 1) / bs, b = pos / bs;
+            const int pos = c + t - s_tok[r], held = (c + bs - 1) >> lbs, b = pos >> lbs;
             const int block = b < held ? g.table[(size_t)r * g.max_blocks + b] : g.free_blocks[s_new[r] + b - held];
-            slot = block * bs + pos - b * bs;
+            slot = block * bs + (pos & (bs - 1));
         }
         g.slots[t] = slot;
     }

@@ -173,7 +173,8 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(const bf16_t* __restric
 
 template <int HD>
 hipError_t launch_append(hipStream_t st, const bf16_t* qkv, const int* slots, int T, int Hq, const Kv8Cache& c) {
-    const int range = (long)T * c.Hkv * 2 <= 16384 ? 1 : 4;
+    // Rows looked at per wave: one while the chip holds a wave per row, else as many as leave it 4096 waves.
+    const int range = (int)std::min(std::max((long)T * c.Hkv * 2 / 4096, 1L), (long)c.block_size);
     const dim3 grid((unsigned)(((long)T + 4 * range - 1) / (4 * range)), c.Hkv * 2);
     switch (c.block_size) {
         case 16: kv8_append_kernel<HD, 16><<<grid, 256, 0, st>>>(qkv, slots, T, range, Hq, c); break;
@@ -206,7 +207,7 @@ __device__ __forceinline__ bf16x8_t bf16_of_codes(uint32_t a, uint32_t b, float 
 }
 
 template <int HD>
-__global__ __launch_bounds__(NW8 * 64) void kv8_attn_kernel(const bf16_t* __restrict__ qkv, Kv8Cache c, const int* __restrict__ table,
+__global__ __launch_bounds__(NW8 * 64, 3) void kv8_attn_kernel(const bf16_t* __restrict__ qkv, Kv8Cache c, const int* __restrict__ table,
                                                             const int* __restrict__ kv_len, bf16_t* __restrict__ o,
                                                             float* __restrict__ part, int lbs, int max_blocks, int Hq, int splits,
                                                             int per, float scale_log2e) {
@@ -216,11 +217,12 @@ __global__ __launch_bounds__(NW8 * 64) void kv8_attn_kernel(const bf16_t* __rest
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, g = lane >> 4;
     const int Hkv = c.Hkv, grp = Hq / Hkv, ngb = (grp + 15) / 16;
-    const int split = blockIdx.x, hk = blockIdx.y / ngb, h0 = (blockIdx.y % ngb) * 16, b = blockIdx.z;
+    // Heads first: ids go round the eight XCDs, and heads have the same work, which requests and pieces have not (with the
+    // pieces first, eight of them to a request, one XCD had all the first pieces and another all the last: 89 us for 64
+    // requests of 300 to 6000 positions, 8 heads of 128; so 57).  Last pieces, which may be empty, come last.
+    const int hk = blockIdx.x / ngb, h0 = (blockIdx.x % ngb) * 16, b = blockIdx.y, split = blockIdx.z;
     const int bs = 1 << lbs;
-    const int n = min(max(kv_len[b], 0), max_blocks << lbs);
-    const int s0 = split * per, s1 = min(n, s0 + per);
-    if (splits > 1 && s0 >= n && split > 0) return;      // the combination reads ceil(n / per) pieces, at least one
+    const int s0 = split * per;
     const int heads = min(grp - h0, 16);
     const int hq = hk * grp + h0;
 
@@ -233,30 +235,47 @@ __global__ __launch_bounds__(NW8 * 64) void kv8_attn_kernel(const bf16_t* __rest
             for (int s = 0; s < 2; ++s) qf[j][s] = *reinterpret_cast<const bf16x8_t*>(qp + j * 64 + s * 8);
     }
     const int* row = table + (size_t)b * max_blocks;
-    f32x4_t acc[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    float m_run = -3.402823466e38f, l_run = 0.f;
-    for (int t0 = s0 + w * 64; t0 < s1; t0 += NW8 * 64) {
-        // the block that holds the positions t0 + 16 x .. of a group x of 16; nothing where there are none or the entry is no block
-        auto block_of = [&](int x, bool* ok) {
-            const int t = t0 + 16 * x;
-            const int k = row[min(t, n - 1) >> lbs];
-            *ok = t < n && (unsigned)k < (unsigned)c.blocks;
-            return (size_t)(*ok ? k : 0) * Hkv + hk;
-        };
-        bool ok_k, ok_v;
-        const size_t bk = block_of(r >> 2, &ok_k), bv = block_of(g, &ok_v);
-        const uint8_t* kp = c.k8 + (bk << lbs) * HD + (((t0 + 16 * (r >> 2)) & (bs - 1)) + (r & 3)) * HD + g * 16;
-        const uint8_t* vp = c.v8 + (bv << lbs) * HD + (r << lbs) + ((t0 + 16 * g) & (bs - 1));
-        const float2 sc = *reinterpret_cast<const float2*>(c.scales + bv * 2);
-        u32x4_t kw[4][NJ], vw[NT];
+    // What a step of 64 positions at t0 reads: its entries of the table first, one step ahead of the rest (K: of the group
+    // that this lane's row of a score tile belongs to, V: of the lane's own group; nothing where there are no positions or
+    // the entry is no block).
+    // An entry behind the last position may be anything: what it leads to is inside the pool and is not looked at.  (Its
+    // load does not wait for kv_len then.)
+    auto entry = [&](int t0, int x) { return row[min((t0 + 16 * x) >> lbs, max_blocks - 1)]; };
+    u32x4_t kw[4][NJ], vw[NT];
+    auto load_k = [&](int t0, int k) {
+        const size_t blk = (size_t)((unsigned)k < (unsigned)c.blocks ? k : 0) * Hkv + hk;
+        const uint8_t* kp = c.k8 + (blk << lbs) * HD + (((t0 + 16 * (r >> 2)) & (bs - 1)) + (r & 3)) * HD + g * 16;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int j = 0; j < NJ; ++j) kw[t][j] = *reinterpret_cast<const u32x4_t*>(kp + t * 4 * HD + j * 64);
+    };
+    float2 sc;
+    auto load_v = [&](int t0, int k) {
+        const size_t blk = (size_t)((unsigned)k < (unsigned)c.blocks ? k : 0) * Hkv + hk;
+        const uint8_t* vp = c.v8 + (blk << lbs) * HD + (r << lbs) + ((t0 + 16 * g) & (bs - 1));
+        sc = *reinterpret_cast<const float2*>(c.scales + blk * 2);
 #pragma unroll
         for (int t = 0; t < NT; ++t) vw[t] = *reinterpret_cast<const u32x4_t*>(vp + ((t * 16) << lbs));
+    };
+    f32x4_t acc[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float m_run = -3.402823466e38f, l_run = 0.f;
+    constexpr int STEP = NW8 * 64;
+    int t0 = s0 + w * 64;
+    int ev = entry(t0, g), ek = entry(t0, r >> 2), ek_next = entry(t0 + STEP, r >> 2), ev_next = entry(t0 + STEP, g);
+    const int n = min(max(kv_len[b], 0), max_blocks << lbs), s1 = min(n, s0 + per);
+    if (s0 >= n && split > 0) return;      // the combination reads ceil(n / per) pieces, at least one
+    if (t0 < s1) {
+        load_k(t0, ek);
+        load_v(t0, ev);
+    }
+    for (; t0 < s1; t0 += STEP) {
+        // Loads return in order: the entries of the step after next go out in front of the next step's rows, so that waiting for
+        // them does not wait for those.
+        const int ek_after = entry(t0 + 2 * STEP, r >> 2), ev_after = entry(t0 + 2 * STEP, g);
+        __builtin_amdgcn_sched_barrier(0);
         f32x4_t s[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -267,8 +286,13 @@ __global__ __launch_bounds__(NW8 * 64) void kv8_attn_kernel(const bf16_t* __rest
                 s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of_codes(kw[t][j][2], kw[t][j][3], 1.0f), qf[j][1], s[t], 0, 0, 0);
             }
         }
-        const int left = ok_v ? min(max(n - (t0 + 16 * g), 0), 16) : 0;      // positions of this lane's 16
-        const float sk = sc.x * scale_log2e;
+        // the next step's keys are on their way while this step's softmax and values are worked, its values during the
+        // next step's keys
+        const bool more = t0 + STEP < s1;
+        if (more) load_k(t0 + STEP, ek_next);
+        const bool ok = (unsigned)ev < (unsigned)c.blocks;
+        const int left = ok ? min(max(n - (t0 + 16 * g), 0), 16) : 0;      // positions of this lane's 16
+        const float sk = sc.x * scale_log2e, sv = left ? sc.y : 1.0f;
         float mx = -INFINITY;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -305,12 +329,13 @@ __global__ __launch_bounds__(NW8 * 64) void kv8_attn_kernel(const bf16_t* __rest
                     vw[t][k] &= live == 4 ? 0xffffffffu : (1u << (8 * live)) - 1;
                 }
         }
-        const float sv = left ? sc.y : 1.0f;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of_codes(vw[t][0], vw[t][1], sv), pf[0], acc[t], 0, 0, 0);
             acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of_codes(vw[t][2], vw[t][3], sv), pf[1], acc[t], 0, 0, 0);
         }
+        if (more) load_v(t0 + STEP, ev_next);
+        ev = ev_next; ev_next = ev_after; ek_next = ek_after;
     }
     l_run += __shfl_xor(l_run, 16, 64);
     l_run += __shfl_xor(l_run, 32, 64);
@@ -340,32 +365,71 @@ __global__ __launch_bounds__(NW8 * 64) void kv8_attn_kernel(const bf16_t* __rest
     }
 }
 
-// o from the pieces of a request's positions, in their order.
-template <int HD>
-__global__ __launch_bounds__(HD) void kv8_combine_kernel(const float* __restrict__ part, const int* __restrict__ kv_len,
-                                                         bf16_t* __restrict__ o, int splits, int per, int most, int Hq) {
-    const int hq = blockIdx.x, b = blockIdx.y, d = threadIdx.x;
-    const int pieces = max((min(max(kv_len[b], 0), most) + per - 1) / per, 1);
+// o from the pieces of a request's positions: NW waves share out the pieces of a head, eight rows in flight each (one chain
+// of dependent loads per piece took 31 us for 59 pieces), and add up in wave order.
+template <int HD, int NW>
+__global__ __launch_bounds__(256) void kv8_combine_kernel(const float* __restrict__ part, const int* __restrict__ kv_len,
+                                                          bf16_t* __restrict__ o, int splits, int per, int most, int Hq) {
+    constexpr int E = HD / 64, BATCH = 8, HEADS = 4 / NW;
+    __shared__ float sums[4][HD];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wave % NW;
+    const int hq = blockIdx.x * HEADS + wave / NW, b = blockIdx.y;
+    const int pieces = hq < Hq ? max((min(max(kv_len[b], 0), most) + per - 1) / per, 1) : 0;
     const float* p = part + ((size_t)b * Hq + hq) * splits * (HD + 2);
-    float M = -INFINITY, L = 0.f, a = 0.f;
-    for (int s = 0; s < pieces; ++s) M = fmaxf(M, p[s * (HD + 2) + HD]);
-    for (int s = 0; s < pieces; ++s) {
-        const float f = __builtin_amdgcn_exp2f(p[s * (HD + 2) + HD] - M);
-        L = fmaf(f, p[s * (HD + 2) + HD + 1], L);
-        a = fmaf(f, p[s * (HD + 2) + d], a);
+    auto ml_of = [&](int s) { return s < pieces ? *reinterpret_cast<const float2*>(p + (size_t)s * (HD + 2) + HD) : make_float2(-INFINITY, 0.f); };
+    float M = -INFINITY, L = 0.f;
+    for (int s = lane; s < pieces; s += 64) M = fmaxf(M, ml_of(s).x);
+    M = wave_max(M);                   // finite: a piece's maximum is never below the lowest finite value
+    for (int s = lane; s < pieces; s += 64) {
+        const float2 ml = ml_of(s);
+        L = fmaf(__builtin_amdgcn_exp2f(ml.x - M), ml.y, L);
     }
-    o[((size_t)b * Hq + hq) * HD + d] = f2bf(L == 0.f ? 0.f : a / L);
+    L = wave_sum(L);
+    float a[E] = {};
+    for (int s0 = w; s0 < pieces; s0 += NW * BATCH) {
+        float v[BATCH][E], f[BATCH];
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+            const int s = min(s0 + NW * k, pieces - 1);
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[k][e] = p[(size_t)s * (HD + 2) + lane + 64 * e];
+            f[k] = ml_of(s0 + NW * k).x;
+        }
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k)
+            if (s0 + NW * k < pieces) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) a[e] = fmaf(__builtin_amdgcn_exp2f(f[k] - M), v[k][e], a[e]);
+            }
+    }
+    const float inv = L == 0.f ? 0.f : 1.0f / L;
+    if (NW == 1) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (hq < Hq) o[((size_t)b * Hq + hq) * HD + lane + 64 * e] = f2bf(a[e] * inv);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) sums[wave][lane + 64 * e] = a[e];
+    __syncthreads();
+    if (threadIdx.x < HD) {
+        const float v = (sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]);
+        o[((size_t)b * Hq + hq) * HD + threadIdx.x] = f2bf(v * inv);
+    }
 }
 
+// Pieces of 768 positions where that is three rounds of work-groups and more (three live on a CU), of 512 where it fills the
+// chip, else of 256; none where the heads alone fill the chip and nobody has more than 1024 positions (the second launch
+// would cost more).  us without the combination's 4 to 5, 64 requests of 300 to 6000 positions with 8 heads of 128 in pieces of
+// 256, 512, 768, 1024, 1536: 66.1 58.8 57.6 59.0 61.7;  30011 and 17003 positions: 20.5 19.2 20.0 19.4 23.3.
 struct Kv8Plan { int splits, per; };
 
 Kv8Plan plan_kv8(int B, int max_blocks, int block_size, int Hq, int Hkv) {
     const long most = (long)max_blocks * block_size;
     const int grp = Hq / Hkv;
     const long groups = (long)B * Hkv * ((grp + 15) / 16);
-    const long splits = std::max(std::min((2048 + groups - 1) / groups, (most + 511) / 512), 1L);
     Kv8Plan p;
-    p.per = (int)(((most + splits - 1) / splits + 255) / 256 * 256);
+    p.per = groups >= 512 && most <= 1024 ? 1024 : groups * most >= 1536L * 768 ? 768 : groups * most >= 512L * 512 ? 512 : 256;
     p.splits = (int)((most + p.per - 1) / p.per);
     return p;
 }
@@ -376,11 +440,14 @@ hipError_t launch_kv8(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* part,
     const Kv8Plan p = plan_kv8(B, max_blocks, c.block_size, Hq, c.Hkv);
     const int lbs = c.block_size == 16 ? 4 : c.block_size == 32 ? 5 : 6, grp = Hq / c.Hkv;
     if (p.splits > 1 && !part) return hipErrorInvalidValue;
-    kv8_attn_kernel<HD><<<dim3(p.splits, c.Hkv * ((grp + 15) / 16), B), NW8 * 64, 0, st>>>(
+    kv8_attn_kernel<HD><<<dim3(c.Hkv * ((grp + 15) / 16), B, p.splits), NW8 * 64, 0, st>>>(
         qkv, c, table, kv_len, o, part, lbs, max_blocks, Hq, p.splits, p.per, 1.4426950408889634f / sqrtf((float)HD));
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
-    kv8_combine_kernel<HD><<<dim3(Hq, B), HD, 0, st>>>(part, kv_len, o, p.splits, p.per, max_blocks << lbs, Hq);
+    if (p.splits > 16)
+        kv8_combine_kernel<HD, 4><<<dim3(Hq, B), 256, 0, st>>>(part, kv_len, o, p.splits, p.per, max_blocks << lbs, Hq);
+    else
+        kv8_combine_kernel<HD, 1><<<dim3((Hq + 3) / 4, B), 256, 0, st>>>(part, kv_len, o, p.splits, p.per, max_blocks << lbs, Hq);
     return hipGetLastError();
 }
 
