@@ -1,100 +1,50 @@
 // Attention over packed prompts: o = softmax(q k^T / sqrt(hd) + mask) v inside each of n sequences whose rows lie one
 // behind the other, causal or bidirectional, grouped heads, head_dim in {64, 80, 128}.
 //
-// The products, the LDS tiles and the softmax in base 2 with a lazily moving reference are those of k_attn.hip.  A wave
-// owns MQ blocks of 32 queries; each key or value fragment that it reads from LDS serves all of them.  The denominator
-// is the fp32 sum of the unrounded probabilities at every head_dim, so that the log-sum-exp is as exact as fp32 allows.
-// A row of scores that are all -inf gives NaN, as the definition does (0 / 0).
+// As in k_attn.hip the scores are formed transposed, S^T = K Q^T (v_mfma_f32_32x32x16_bf16: a lane holds one query and 16 keys
+// of a 32-key step), and the probabilities in bf16 are the B operand of O^T = V^T P^T as they stand; tiles of 64 keys come
+// by LDS-DMA and V^T out of the transposing LDS read.
+//
+// What bounds such a kernel: a 32-query wave reads 1 KB of LDS per MFMA of 32 cycles, which for the four SIMDs of a CU is all
+// that its LDS delivers, and the softmax arithmetic takes as many cycles on the vector pipe as the products take on the
+// matrix pipe.
+//
+// The denominator is the fp32 sum of the unrounded probabilities, so that the log-sum-exp is as exact as fp32 allows.  A
+// row of scores that are all -inf gives NaN, as the definition does (0 / 0).
 #include "sp_attn.h"
 #include "sp_packed.h"
 
 namespace {
 
-// One tile of 64 keys for one wave's MQ x 32 queries.
-template <int HD, int NW, int MQ, bool MASK>
-__device__ __forceinline__ void packed_tile(const unsigned char* sK, const unsigned char* sV, const int* kpos, const int* vpos,
-                                            const bf16x8_t (*qf)[HD / 16], f32x16_t (*oacc)[(HD + 31) / 32], float* m_run, float* l_run,
-                                            int key0, int len, int causal, int qi, int half, float scale_log2e) {
-    typedef AttnCfg<HD, NW> C;
-    f32x16_t sacc[MQ][2];
-#pragma unroll
-    for (int m = 0; m < MQ; ++m)
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) sacc[m][t][e] = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < C::NKS; ++ks)
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(sK + t * 32 * C::ROWB + kpos[ks]);
-#pragma unroll
-            for (int m = 0; m < MQ; ++m) sacc[m][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[m][ks], sacc[m][t], 0, 0, 0);
-        }
-    bf16x8_t pf[MQ][2][2];
-#pragma unroll
-    for (int m = 0; m < MQ; ++m) {
-        if (MASK) {
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int key = key0 + t * 32 + (e >> 2) * 8 + half * 4 + (e & 3);
-                    if (key >= len || (causal && key > qi + 32 * m)) sacc[m][t][e] = -INFINITY;
-                }
-        }
-        float mx = -INFINITY;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sacc[m][t][e]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        // the reference starts at the lowest finite value: a tile without a visible key then has probabilities 0
-        const bool move = (mx - m_run[m]) * scale_log2e > 8.0f;
-        const float m_new = move ? mx : m_run[m];
-        const float alpha = move ? __builtin_amdgcn_exp2f((m_run[m] - m_new) * scale_log2e) : 1.0f;
-        const float m_scaled = m_new * scale_log2e;
-        m_run[m] = m_new;
-        float psum = 0.f;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float p = __builtin_amdgcn_exp2f(fmaf(sacc[m][t][j * 8 + e], scale_log2e, -m_scaled));
-                    psum += p;
-                    pf[m][t][j][e] = (__bf16)p;      // at most 256: half a step of bf16, as every operand of the products
-                }
-        l_run[m] = l_run[m] * alpha + psum;
-        if (__any(move)) {
-#pragma unroll
-            for (int t = 0; t < C::NMT; ++t)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) oacc[m][t][e] *= alpha;
-        }
-    }
-#pragma unroll
-    for (int tj = 0; tj < 4; ++tj)
-#pragma unroll
-        for (int mt = 0; mt < C::NMT; ++mt) {
-            const unsigned char* vp = sV + ((tj >> 1) * 32 + 16 * (tj & 1)) * C::ROWB + vpos[mt];
-            const s16x4_t lo = sp_tr_read((lds_s16x4_ptr)(vp));
-            const s16x4_t hi = sp_tr_read((lds_s16x4_ptr)(vp + 8 * C::ROWB));
-            const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, s16x8_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
-#pragma unroll
-            for (int m = 0; m < MQ; ++m) oacc[m][mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[m][tj >> 1][tj & 1], oacc[m][mt], 0, 0, 0);
-        }
+__device__ __forceinline__ bf16x8_t lds_frag(const unsigned char* __restrict__ p) { return *reinterpret_cast<const bf16x8_t*>(p); }
+
+// Maximum of a value over the two half-waves.
+__device__ __forceinline__ float half_max(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-template <int HD, int NW, int MQ>
-__global__ __launch_bounds__(NW * 64, MQ == 1 ? 2 : 1) void attn_packed_kernel(const bf16_t* __restrict__ qkv, const int* __restrict__ cu,
-                                                                              bf16_t* __restrict__ o, float* __restrict__ lse, int n,
-                                                                              int T, int slots, int Hq, int Hkv, int causal,
-                                                                              float scale_log2e) {
+template <int HD>
+struct PackedCfg {
+#ifndef PNW
+#define PNW 8
+#define PMQ 1
+#endif
+    static constexpr int NW = PNW, MQ = PMQ, QB = NW * MQ * 32;
     typedef AttnCfg<HD, NW> C;
-    constexpr int QB = NW * MQ * 32;
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem_packed[];     // two stages of {K tile, V tile}
+    static constexpr int STAGES = 3;       // the keys of a tile are read beside the values of the one before, the loads run another one ahead
+    static constexpr int LDS = STAGES * C::STAGE;
+    static_assert(LDS <= 160 * 1024, "fits the LDS");
+};
+
+template <int HD>
+__global__ __launch_bounds__(64 * PackedCfg<HD>::NW, PackedCfg<HD>::NW / 4) void attn_packed_kernel(const bf16_t* __restrict__ qkv, const int* __restrict__ cu,
+                                                           bf16_t* __restrict__ o, float* __restrict__ lse, int n, int T, int slots,
+                                                           int Hq, int Hkv, int causal, float scale_log2e) {
+    typedef PackedCfg<HD> G;
+    typedef typename G::C C;
+    constexpr int MQ = G::MQ, QB = G::QB;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem_packed[];     // stages of {K tile, V tile}
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, half = lane >> 5;
     // An XCD works through a contiguous range of (head, slot): a head's keys and values come through one L2, and every XCD
@@ -106,8 +56,10 @@ __global__ __launch_bounds__(NW * 64, MQ == 1 ? 2 : 1) void attn_packed_kernel(c
     const int len = pb.len, ld = (Hq + 2 * Hkv) * HD;
     const size_t tok0 = pb.row0;
     [[maybe_unused]] const bf16_t* kbase = qkv + tok0 * ld + (size_t)(Hq + h / (Hq / Hkv)) * HD;
-    int ld_col[C::NLOAD], ld_row[C::NLOAD];
-    bool ld_on[C::NLOAD];
+    // Instruction i of a wave lands at byte (wave * NLOAD + i) * 1024 + lane * 16 of a stage; the lane fetches the chunk that the
+    // swizzle puts there, as a byte offset from the tile's first key.  Rows behind the sequence and the padding of the
+    // 192-byte rows lie outside the buffer that a load is given and land as zeros.
+    uint32_t ld_off[C::NLOAD];
 #pragma unroll
     for (int i = 0; i < C::NLOAD; ++i) {
         const int off = (wave * C::NLOAD + i) * 1024 + lane * 16;
@@ -115,25 +67,27 @@ __global__ __launch_bounds__(NW * 64, MQ == 1 ? 2 : 1) void attn_packed_kernel(c
         const int rel = off - (isv ? C::TILE_BYTES : 0);
         const int row = rel / C::ROWB, pos = (rel % C::ROWB) >> 4;
         const int c = isv ? pos ^ (C::v_swz(row) << 2) : pos ^ C::k_swz(row);
-        ld_on[i] = c < C::CPR;
-        ld_row[i] = row;
-        ld_col[i] = (isv ? Hkv * HD : 0) + (c < C::CPR ? c : 0) * 8;
+        ld_off[i] = c < C::CPR ? (uint32_t)(row * ld + (isv ? Hkv * HD : 0) + c * 8) * 2 : 0xffffffffu;
     }
-    auto issue = [&](int kt) {
+    auto issue = [&](int kt, int stage) __attribute__((always_inline)) {
 #if defined(__HIP_DEVICE_COMPILE__)
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(kbase + (size_t)kt * KB * ld), 0, min(len - kt * KB, KB) * ld * 2,
+                                                            0x00020000);
 #pragma unroll
         for (int i = 0; i < C::NLOAD; ++i)
-            if (wave * C::NLOAD + i < C::NINST && ld_on[i])
-                __builtin_amdgcn_global_load_lds(kbase + ((size_t)min(kt * KB + ld_row[i], len - 1) * ld + ld_col[i]),
-                                                 (lds_void_ptr)(smem_packed + (kt & 1) * C::STAGE + (wave * C::NLOAD + i) * 1024), 16, 0, 0);
+            if (wave * C::NLOAD + i < C::NINST)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void_ptr)(smem_packed + stage * C::STAGE + (wave * C::NLOAD + i) * 1024), 16,
+                                                         ld_off[i], 0, 0, 0);
 #endif
     };
-    int kpos[C::NKS], vpos[C::NMT];
-#pragma unroll
-    for (int ks = 0; ks < C::NKS; ++ks) kpos[ks] = l32 * C::ROWB + (((2 * ks + half) ^ C::k_swz(l32)) << 4);
+    // Lane parts of the fragment addresses.  Rows of 128 and 256 bytes: a k-step, or a 32-row block of V^T, is an exclusive or
+    // on top; rows of 192: two k-steps of four chunks are an offset.
+    constexpr bool XOR = HD != 80;
+    const int kp0 = l32 * C::ROWB + ((half ^ C::k_swz(l32)) << 4), kp1 = l32 * C::ROWB + (((2 | half) ^ C::k_swz(l32)) << 4);
+    auto k_at = [&](int base, int ks) { return XOR ? (base + kp0) ^ (ks << 5) : base + ((ks & 1) ? kp1 : kp0) + (ks >> 1) * 64; };
     const int rowv = half * 4 + ((lane & 15) >> 2);
-#pragma unroll
-    for (int mt = 0; mt < C::NMT; ++mt) vpos[mt] = rowv * C::ROWB + ((mt ^ C::v_swz(rowv)) << 6) + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+    const int vp0 = rowv * C::ROWB + (C::v_swz(rowv) << 6) + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+    auto v_at = [&](int base, int mt) { return XOR ? (base + vp0) ^ (mt << 6) : base + vp0 + mt * 64; };
 
     const int q0 = pb.blk * QB, wq0 = q0 + wave * (MQ * 32), qi = wq0 + l32;
     bf16x8_t qf[MQ][C::NKS];
@@ -147,34 +101,133 @@ __global__ __launch_bounds__(NW * 64, MQ == 1 ? 2 : 1) void attn_packed_kernel(c
     float m_run[MQ], l_run[MQ];
 #pragma unroll
     for (int m = 0; m < MQ; ++m) {
-        m_run[m] = -3.402823466e38f;
+        m_run[m] = -3.402823466e38f;       // finite: a step without a visible key then has probabilities 0
         l_run[m] = 0.f;
 #pragma unroll
         for (int t = 0; t < C::NMT; ++t)
 #pragma unroll
             for (int e = 0; e < 16; ++e) oacc[m][t][e] = 0.f;
     }
-    const int k_end = causal ? min(len, q0 + QB) : len;
-    const int ntiles = (k_end + KB - 1) / KB;
-    auto landed = [&] {     // this wave's loads; behind the barrier every wave's, and every wave is done with the other stage
+    const int ntiles = ((causal ? min(len, q0 + QB) : len) + KB - 1) / KB;               // of the work-group
+    const int mine = wq0 >= len ? 0 : ((causal ? min(len, wq0 + MQ * 32) : len) + KB - 1) / KB;   // of this wave
+
+    auto scores = [&](int base, f32x16_t (&s)[MQ]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int ks = 0; ks < C::NKS; ++ks) {
+            const bf16x8_t kf = lds_frag(smem_packed + k_at(base, ks));
+#pragma unroll
+            for (int m = 0; m < MQ; ++m) {
+                if (ks == 0)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[m][e] = 0.f;
+                s[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[m][ks], s[m], 0, 0, 0);
+            }
+        }
+    };
+    auto output = [&](int base, const bf16x8_t (&p)[MQ][2]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int mt = 0; mt < C::NMT; ++mt) {
+                const unsigned char* vp = smem_packed + v_at(base, mt) + 16 * j * C::ROWB;
+                const s16x4_t lo = sp_tr_read((lds_s16x4_ptr)(vp));
+                const s16x4_t hi = sp_tr_read((lds_s16x4_ptr)(vp + 8 * C::ROWB));
+                const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, s16x8_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+#pragma unroll
+                for (int m = 0; m < MQ; ++m) oacc[m][mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[m][j], oacc[m][mt], 0, 0, 0);
+            }
+    };
+    // probabilities of the 32 keys from key0 on; returns whether a reference moved, and by which factor
+    auto soften = [&](f32x16_t (&s)[MQ], bf16x8_t (&p)[MQ][2], float (&alpha)[MQ], int key0, bool mask) __attribute__((always_inline)) {
+        bool any = false;
+#pragma unroll
+        for (int m = 0; m < MQ; ++m) {
+            if (mask) {
+                // element e is key key0 + 4 half + (e >> 2) * 8 + (e & 3)
+                const int last = min(len - 1, causal ? qi + 32 * m : len - 1) - key0 - 4 * half;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[m][e] = (e >> 2) * 8 + (e & 3) <= last ? s[m][e] : -INFINITY;
+            }
+            float mx = s[m][0];
+#pragma unroll
+            for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[m][e]);
+            mx = half_max(mx);
+            // the reference follows the maximum lazily, see k_attn.hip
+            const bool move = (mx - m_run[m]) * scale_log2e > 8.0f;
+            const float m_new = move ? mx : m_run[m];
+            alpha[m] = move ? __builtin_amdgcn_exp2f((m_run[m] - m_new) * scale_log2e) : 1.0f;
+            const float m_scaled = m_new * scale_log2e;
+            m_run[m] = m_new;
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const float v = __builtin_amdgcn_exp2f(fmaf(s[m][e], scale_log2e, -m_scaled));
+                sum += v;
+                p[m][e >> 3][e & 7] = (__bf16)v;         // at most 256: half a step of bf16, as every operand of the products
+            }
+            l_run[m] = fmaf(l_run[m], alpha[m], sum);
+            any |= move;
+        }
+        return any;
+    };
+    f32x16_t sa[MQ], sb[MQ];
+    bf16x8_t p[MQ][2];
+    float alpha[MQ];
+    auto rescale = [&](bool any) __attribute__((always_inline)) {
+        if (__any(any)) {
+#pragma unroll
+            for (int m = 0; m < MQ; ++m) {
+                float f = alpha[m];
+                asm volatile("" : "+v"(f));          // keeps the products here: speculated they cost their time in every step, and 64 registers
+#pragma unroll
+                for (int t = 0; t < C::NMT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) oacc[m][t][e] *= f;
+            }
+        }
+    };
+    constexpr int HALF = 32 * C::ROWB;
+    // Tile kt: the scores of its second half beside the softmax of its first, then the next tile's first scores (of whatever
+    // the stage holds behind the last one: not used) beside the softmax of the second half.
+    auto body = [&](int cur, int next, int key0, bool mask) __attribute__((always_inline)) {
+        scores(cur + HALF, sb);
+        bool any = soften(sa, p, alpha, key0, mask);
+        rescale(any);
+        output(cur + C::TILE_BYTES, p);
+        scores(next, sa);
+        any = soften(sb, p, alpha, key0 + 32, mask);
+        rescale(any);
+        output(cur + C::TILE_BYTES + HALF, p);
+    };
+    int st0 = 0, st1 = 1, st2 = 2;           // stages of the tiles kt, kt + 1, kt + 2
+    auto enter = [&](int kt) __attribute__((always_inline)) {
+        // tiles kt and kt + 1 have landed, this wave's part by the wait, everybody's by the barrier; and everybody is
+        // done with tile kt - 1, whose stage tile kt + 2 takes
         __builtin_amdgcn_s_waitcnt(sp_waitcnt(0, 15));
         asm volatile("" ::: "memory");
-        __syncthreads();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (kt + 2 < ntiles) issue(kt + 2, st2);
     };
-    issue(0);
-    landed();
-    for (int kt = 0; kt < ntiles; ++kt) {
-        const int key0 = kt * KB;
-        if (kt + 1 < ntiles) issue(kt + 1);
-        const unsigned char* sK = smem_packed + (kt & 1) * C::STAGE;
-        // wave-uniform: no key of the tile is visible to the wave, no query of the wave exists
-        if (!((causal && key0 > wq0 + MQ * 32 - 1) || wq0 >= len)) {
-            if ((causal && key0 + KB - 1 > wq0) || key0 + KB > len)
-                packed_tile<HD, NW, MQ, true>(sK, sK + C::TILE_BYTES, kpos, vpos, qf, oacc, m_run, l_run, key0, len, causal, qi, half, scale_log2e);
-            else
-                packed_tile<HD, NW, MQ, false>(sK, sK + C::TILE_BYTES, kpos, vpos, qf, oacc, m_run, l_run, key0, len, causal, qi, half, scale_log2e);
+    auto rotate = [&] { const int t = st0; st0 = st1; st1 = st2; st2 = t; };
+    issue(0, 0);
+    if (ntiles > 1) issue(1, 1);
+    // One barrier per tile for every wave, whatever it has to do in it.  The diagonal and a ragged end lie in a wave's last
+    // tile: it alone is masked, outside the loop.
+    int kt = 0;
+    enter(0);
+    if (mine > 0) {
+        scores(0, sa);
+        for (; kt + 1 < mine;) {
+            body(st0 * C::STAGE, st1 * C::STAGE, kt * KB, false);
+            rotate();
+            enter(++kt);
         }
-        if (kt + 1 < ntiles) landed();
+        body(st0 * C::STAGE, st1 * C::STAGE, kt * KB, true);
+    }
+    while (kt + 1 < ntiles) {
+        rotate();
+        enter(++kt);
     }
 #pragma unroll
     for (int m = 0; m < MQ; ++m) {
@@ -197,15 +250,15 @@ __global__ __launch_bounds__(NW * 64, MQ == 1 ? 2 : 1) void attn_packed_kernel(c
     }
 }
 
-template <int HD, int NW, int MQ>
+template <int HD>
 hipError_t launch_packed(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* lse, const PackedShape& a) {
-    constexpr int LDS = 2 * AttnCfg<HD, NW>::STAGE;
+    typedef PackedCfg<HD> G;
     static LdsLimitOnce lds_limit;
-    hipError_t e = lds_limit.set(reinterpret_cast<const void*>(attn_packed_kernel<HD, NW, MQ>), LDS);
+    hipError_t e = lds_limit.set(reinterpret_cast<const void*>(attn_packed_kernel<HD>), G::LDS);
     if (e != hipSuccess) return e;
-    const int slots = a.T / (NW * MQ * 32) + a.n;
-    attn_packed_kernel<HD, NW, MQ><<<dim3((unsigned)((long)slots * a.Hq)), NW * 64, LDS, st>>>(qkv, a.cu, o, lse, a.n, a.T, slots, a.Hq, a.Hkv,
-                                                                                               a.causal, 1.4426950408889634f / sqrtf((float)HD));
+    const int slots = a.T / G::QB + a.n;
+    attn_packed_kernel<HD><<<dim3((unsigned)((long)slots * a.Hq)), 64 * G::NW, G::LDS, st>>>(qkv, a.cu, o, lse, a.n, a.T, slots, a.Hq, a.Hkv,
+                                                                                             a.causal, 1.4426950408889634f / sqrtf((float)HD));
     return hipGetLastError();
 }
 
@@ -213,9 +266,9 @@ hipError_t launch_packed(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* ls
 
 hipError_t spk_launch_attention_packed(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* lse, const PackedShape& a) {
     switch (a.hd) {
-        case 64: return launch_packed<64, 4, 1>(st, qkv, o, lse, a);
-        case 80: return launch_packed<80, 4, 1>(st, qkv, o, lse, a);
-        case 128: return launch_packed<128, 4, 1>(st, qkv, o, lse, a);
+        case 64: return launch_packed<64>(st, qkv, o, lse, a);
+        case 80: return launch_packed<80>(st, qkv, o, lse, a);
+        case 128: return launch_packed<128>(st, qkv, o, lse, a);
         default: return hipErrorInvalidValue;
     }
 }
