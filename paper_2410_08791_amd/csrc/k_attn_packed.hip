@@ -39,7 +39,7 @@ struct PackedCfg {
 
 template <int HD>
 __global__ __launch_bounds__(64 * PackedCfg<HD>::NW, PackedCfg<HD>::NW / 4) void attn_packed_kernel(const bf16_t* __restrict__ qkv, const int* __restrict__ cu,
-                                                           bf16_t* __restrict__ o, float* __restrict__ lse, int n, int T, int slots,
+                                                           bf16_t* __restrict__ o, float* __restrict__ lse, int n, int T,
                                                            int Hq, int Hkv, int causal, float scale_log2e) {
     typedef PackedCfg<HD> G;
     typedef typename G::C C;
@@ -47,11 +47,13 @@ __global__ __launch_bounds__(64 * PackedCfg<HD>::NW, PackedCfg<HD>::NW / 4) void
     extern __shared__ __attribute__((aligned(16))) unsigned char smem_packed[];     // stages of {K tile, V tile}
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, half = lane >> 5;
-    // An XCD works through a contiguous range of (head, slot): a head's keys and values come through one L2, and every XCD
-    // gets its share of the long sequences, which it would not if the range ran over the sequences first.
-    const int job = xcd_remap(blockIdx.x, gridDim.x);
-    const int h = job / slots;
-    const PackedBlock pb = packed_block<QB>(cu, n, T, job - h * slots);
+    // Slots first, a slot's heads side by side: work-groups then start in the order of a sequence's blocks, longest first,
+    // for all heads, and what is left for the end is short.  (Head after head, the last head's longest block started when
+    // everything else was all but done.)  Ids go round the eight XCDs, each with its own L2: an XCD gets neighbouring heads,
+    // which share keys and values.
+    const int slot = blockIdx.x / Hq, hi = blockIdx.x - slot * Hq;
+    const int h = Hq & 7 ? hi : (hi & 7) * (Hq >> 3) + (hi >> 3);
+    const PackedBlock pb = packed_block<QB>(cu, n, T, slot);
     if (pb.blk * QB >= pb.len) return;
     const int len = pb.len, ld = (Hq + 2 * Hkv) * HD;
     const size_t tok0 = pb.row0;
@@ -124,21 +126,10 @@ __global__ __launch_bounds__(64 * PackedCfg<HD>::NW, PackedCfg<HD>::NW / 4) void
             }
         }
     };
-    auto output = [&](int base, const bf16x8_t (&p)[MQ][2]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int mt = 0; mt < C::NMT; ++mt) {
-                const unsigned char* vp = smem_packed + v_at(base, mt) + 16 * j * C::ROWB;
-                const s16x4_t lo = sp_tr_read((lds_s16x4_ptr)(vp));
-                const s16x4_t hi = sp_tr_read((lds_s16x4_ptr)(vp + 8 * C::ROWB));
-                const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, s16x8_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
-#pragma unroll
-                for (int m = 0; m < MQ; ++m) oacc[m][mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[m][j], oacc[m][mt], 0, 0, 0);
-            }
-    };
-    // probabilities of the 32 keys from key0 on; returns whether a reference moved, and by which factor
-    auto soften = [&](f32x16_t (&s)[MQ], bf16x8_t (&p)[MQ][2], float (&alpha)[MQ], int key0, bool mask) __attribute__((always_inline)) {
+    f32x16_t sa[MQ], sb[MQ];
+    float alpha[MQ], mx[MQ];                 // mx: of the lane's 16 scores of the next step
+    // Masks the scores of the 32 keys from key0 on, moves the references that they ask for, and rescales what was summed up to them.
+    auto settle = [&](f32x16_t (&s)[MQ], int key0, bool mask) __attribute__((always_inline)) {
         bool any = false;
 #pragma unroll
         for (int m = 0; m < MQ; ++m) {
@@ -147,38 +138,24 @@ __global__ __launch_bounds__(64 * PackedCfg<HD>::NW, PackedCfg<HD>::NW / 4) void
                 const int last = min(len - 1, causal ? qi + 32 * m : len - 1) - key0 - 4 * half;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[m][e] = (e >> 2) * 8 + (e & 3) <= last ? s[m][e] : -INFINITY;
-            }
-            float mx = s[m][0];
+                mx[m] = s[m][0];
 #pragma unroll
-            for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[m][e]);
-            mx = half_max(mx);
+                for (int e = 1; e < 16; ++e) mx[m] = fmaxf(mx[m], s[m][e]);
+            }
+            const float top = half_max(mx[m]);
             // the reference follows the maximum lazily, see k_attn.hip
-            const bool move = (mx - m_run[m]) * scale_log2e > 8.0f;
-            const float m_new = move ? mx : m_run[m];
+            const bool move = (top - m_run[m]) * scale_log2e > 8.0f;
+            const float m_new = move ? top : m_run[m];
             alpha[m] = move ? __builtin_amdgcn_exp2f((m_run[m] - m_new) * scale_log2e) : 1.0f;
-            const float m_scaled = m_new * scale_log2e;
             m_run[m] = m_new;
-            float sum = 0.f;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const float v = __builtin_amdgcn_exp2f(fmaf(s[m][e], scale_log2e, -m_scaled));
-                sum += v;
-                p[m][e >> 3][e & 7] = (__bf16)v;         // at most 256: half a step of bf16, as every operand of the products
-            }
-            l_run[m] = fmaf(l_run[m], alpha[m], sum);
             any |= move;
         }
-        return any;
-    };
-    f32x16_t sa[MQ], sb[MQ];
-    bf16x8_t p[MQ][2];
-    float alpha[MQ];
-    auto rescale = [&](bool any) __attribute__((always_inline)) {
         if (__any(any)) {
 #pragma unroll
             for (int m = 0; m < MQ; ++m) {
                 float f = alpha[m];
                 asm volatile("" : "+v"(f));          // keeps the products here: speculated they cost their time in every step, and 64 registers
+                l_run[m] *= f;
 #pragma unroll
                 for (int t = 0; t < C::NMT; ++t)
 #pragma unroll
@@ -186,18 +163,72 @@ __global__ __launch_bounds__(64 * PackedCfg<HD>::NW, PackedCfg<HD>::NW / 4) void
             }
         }
     };
+    // One step of 32 keys, settled scores s: the next step's scores beside the probabilities of this one, then its output beside
+    // the maximum of the next.  The order is the source's: fragments are read PF ahead of the MFMA that takes them, and each
+    // MFMA is followed by its share of the vector arithmetic (left to the compiler, every read was waited for at once).
+    auto step = [&](f32x16_t (&s)[MQ], int base_v, f32x16_t (&s_next)[MQ], int base_k) __attribute__((always_inline)) {
+        constexpr int PF = 3, NK = C::NKS, NV = 2 * C::NMT;
+        bf16x8_t p[MQ][2], kf[NK], vf[NV];
+        float m_scaled[MQ], sum[MQ];
+        auto kread = [&](int i) __attribute__((always_inline)) { kf[i] = lds_frag(smem_packed + k_at(base_k, i)); };
+        auto vread = [&](int i) __attribute__((always_inline)) {
+            const unsigned char* vp = smem_packed + v_at(base_v, i % C::NMT) + 16 * (i / C::NMT) * C::ROWB;
+            const s16x4_t lo = sp_tr_read((lds_s16x4_ptr)(vp));
+            const s16x4_t hi = sp_tr_read((lds_s16x4_ptr)(vp + 8 * C::ROWB));
+            vf[i] = __builtin_bit_cast(bf16x8_t, s16x8_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+        };
+#pragma unroll
+        for (int i = 0; i < PF; ++i) kread(i);
+#pragma unroll
+        for (int m = 0; m < MQ; ++m) {
+            m_scaled[m] = m_run[m] * scale_log2e;
+            sum[m] = 0.f;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s_next[m][e] = 0.f;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < NK; ++i) {
+            if (i + PF < NK) kread(i + PF);
+            else vread(i + PF - NK);
+#pragma unroll
+            for (int m = 0; m < MQ; ++m) s_next[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[m][i], s_next[m], 0, 0, 0);
+#pragma unroll
+            for (int m = 0; m < MQ; ++m)
+#pragma unroll
+                for (int e = 16 * i / NK; e < 16 * (i + 1) / NK; ++e) {
+                    const float v = __builtin_amdgcn_exp2f(fmaf(s[m][e], scale_log2e, -m_scaled[m]));
+                    sum[m] += v;
+                    p[m][e >> 3][e & 7] = (__bf16)v;         // at most 256: half a step of bf16, as every operand of the products
+                }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int m = 0; m < MQ; ++m) {
+            l_run[m] += sum[m];
+            mx[m] = s_next[m][0];
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (i + PF < NV) vread(i + PF);
+#pragma unroll
+            for (int m = 0; m < MQ; ++m)
+                oacc[m][i % C::NMT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i], p[m][i / C::NMT], oacc[m][i % C::NMT], 0, 0, 0);
+#pragma unroll
+            for (int m = 0; m < MQ; ++m)
+#pragma unroll
+                for (int e = 16 * i / NV; e < 16 * (i + 1) / NV; ++e) mx[m] = fmaxf(mx[m], s_next[m][e]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
     constexpr int HALF = 32 * C::ROWB;
-    // Tile kt: the scores of its second half beside the softmax of its first, then the next tile's first scores (of whatever
-    // the stage holds behind the last one: not used) beside the softmax of the second half.
+    // Tile kt, the scores of whose first half are there: the second half's beside it, then the next tile's (of whatever the stage
+    // holds behind the last one: not used).
     auto body = [&](int cur, int next, int key0, bool mask) __attribute__((always_inline)) {
-        scores(cur + HALF, sb);
-        bool any = soften(sa, p, alpha, key0, mask);
-        rescale(any);
-        output(cur + C::TILE_BYTES, p);
-        scores(next, sa);
-        any = soften(sb, p, alpha, key0 + 32, mask);
-        rescale(any);
-        output(cur + C::TILE_BYTES + HALF, p);
+        settle(sa, key0, mask);
+        step(sa, cur + C::TILE_BYTES, sb, cur + HALF);
+        settle(sb, key0 + 32, mask);
+        step(sb, cur + C::TILE_BYTES + HALF, sa, next);
     };
     int st0 = 0, st1 = 1, st2 = 2;           // stages of the tiles kt, kt + 1, kt + 2
     auto enter = [&](int kt) __attribute__((always_inline)) {
@@ -218,6 +249,12 @@ __global__ __launch_bounds__(64 * PackedCfg<HD>::NW, PackedCfg<HD>::NW / 4) void
     enter(0);
     if (mine > 0) {
         scores(0, sa);
+#pragma unroll
+        for (int m = 0; m < MQ; ++m) {
+            mx[m] = sa[m][0];
+#pragma unroll
+            for (int e = 1; e < 16; ++e) mx[m] = fmaxf(mx[m], sa[m][e]);
+        }
         for (; kt + 1 < mine;) {
             body(st0 * C::STAGE, st1 * C::STAGE, kt * KB, false);
             rotate();
@@ -257,7 +294,7 @@ hipError_t launch_packed(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* ls
     hipError_t e = lds_limit.set(reinterpret_cast<const void*>(attn_packed_kernel<HD>), G::LDS);
     if (e != hipSuccess) return e;
     const int slots = a.T / G::QB + a.n;
-    attn_packed_kernel<HD><<<dim3((unsigned)((long)slots * a.Hq)), 64 * G::NW, G::LDS, st>>>(qkv, a.cu, o, lse, a.n, a.T, slots, a.Hq, a.Hkv,
+    attn_packed_kernel<HD><<<dim3((unsigned)((long)slots * a.Hq)), 64 * G::NW, G::LDS, st>>>(qkv, a.cu, o, lse, a.n, a.T, a.Hq, a.Hkv,
                                                                                              a.causal, 1.4426950408889634f / sqrtf((float)HD));
     return hipGetLastError();
 }
