@@ -16,6 +16,8 @@
 
 namespace {
 
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+
 __device__ __forceinline__ bf16x8_t lds_frag(const unsigned char* __restrict__ p) { return *reinterpret_cast<const bf16x8_t*>(p); }
 
 // Maximum of a value over the two half-waves.
@@ -24,24 +26,20 @@ __device__ __forceinline__ float half_max(float v) {
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-template <int HD>
+template <int HD, int NWAVES>
 struct PackedCfg {
-#ifndef PNW
-#define PNW 8
-#define PMQ 1
-#endif
-    static constexpr int NW = PNW, MQ = PMQ, QB = NW * MQ * 32;
+    static constexpr int NW = NWAVES, MQ = 1, QB = NW * MQ * 32;
     typedef AttnCfg<HD, NW> C;
-    static constexpr int STAGES = 3;       // the keys of a tile are read beside the values of the one before, the loads run another one ahead
+    static constexpr int STAGES = 2;
     static constexpr int LDS = STAGES * C::STAGE;
     static_assert(LDS <= 160 * 1024, "fits the LDS");
 };
 
-template <int HD>
-__global__ __launch_bounds__(64 * PackedCfg<HD>::NW, PackedCfg<HD>::NW / 4) void attn_packed_kernel(const bf16_t* __restrict__ qkv, const int* __restrict__ cu,
+template <int HD, int NW>
+__global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void attn_packed_kernel(const bf16_t* __restrict__ qkv, const int* __restrict__ cu,
                                                            bf16_t* __restrict__ o, float* __restrict__ lse, int n, int T,
                                                            int Hq, int Hkv, int causal, float scale_log2e) {
-    typedef PackedCfg<HD> G;
+    typedef PackedCfg<HD, NW> G;
     typedef typename G::C C;
     constexpr int MQ = G::MQ, QB = G::QB;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem_packed[];     // stages of {K tile, V tile}
@@ -165,10 +163,12 @@ __global__ __launch_bounds__(64 * PackedCfg<HD>::NW, PackedCfg<HD>::NW / 4) void
     };
     // One step of 32 keys, settled scores s: the next step's scores beside the probabilities of this one, then its output beside
     // the maximum of the next.  The order is the source's: fragments are read PF ahead of the MFMA that takes them, and each
-    // MFMA is followed by its share of the vector arithmetic (left to the compiler, every read was waited for at once).
-    auto step = [&](f32x16_t (&s)[MQ], int base_v, f32x16_t (&s_next)[MQ], int base_k) __attribute__((always_inline)) {
+    // MFMA is followed by its share of the vector arithmetic (left to the compiler, every read was waited for at once; the
+    // empty asm statements keep it from sinking the arithmetic to its use).
+    auto step = [&](f32x16_t (&s)[MQ], int base_v, f32x16_t (&s_next)[MQ], int base_k, bool next) __attribute__((always_inline)) {
         constexpr int PF = 3, NK = C::NKS, NV = 2 * C::NMT;
-        bf16x8_t p[MQ][2], kf[NK], vf[NV];
+        u32x4_t p[MQ][2];
+        bf16x8_t kf[NK], vf[NV];
         float m_scaled[MQ], sum[MQ];
         auto kread = [&](int i) __attribute__((always_inline)) { kf[i] = lds_frag(smem_packed + k_at(base_k, i)); };
         auto vread = [&](int i) __attribute__((always_inline)) {
@@ -178,7 +178,8 @@ __global__ __launch_bounds__(64 * PackedCfg<HD>::NW, PackedCfg<HD>::NW / 4) void
             vf[i] = __builtin_bit_cast(bf16x8_t, s16x8_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
         };
 #pragma unroll
-        for (int i = 0; i < PF; ++i) kread(i);
+        for (int i = 0; i < PF; ++i)
+            if (next) kread(i);
 #pragma unroll
         for (int m = 0; m < MQ; ++m) {
             m_scaled[m] = m_run[m] * scale_log2e;
@@ -189,17 +190,21 @@ __global__ __launch_bounds__(64 * PackedCfg<HD>::NW, PackedCfg<HD>::NW / 4) void
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < NK; ++i) {
-            if (i + PF < NK) kread(i + PF);
-            else vread(i + PF - NK);
+            if (i + PF >= NK) vread(i + PF - NK);
+            else if (next) kread(i + PF);
 #pragma unroll
-            for (int m = 0; m < MQ; ++m) s_next[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[m][i], s_next[m], 0, 0, 0);
+            for (int m = 0; m < MQ; ++m)
+                if (next) s_next[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[m][i], s_next[m], 0, 0, 0);
 #pragma unroll
             for (int m = 0; m < MQ; ++m)
 #pragma unroll
-                for (int e = 16 * i / NK; e < 16 * (i + 1) / NK; ++e) {
-                    const float v = __builtin_amdgcn_exp2f(fmaf(s[m][e], scale_log2e, -m_scaled[m]));
-                    sum[m] += v;
-                    p[m][e >> 3][e & 7] = (__bf16)v;         // at most 256: half a step of bf16, as every operand of the products
+                for (int e = 8 * i / NK; e < 8 * (i + 1) / NK; ++e) {
+                    const float v = __builtin_amdgcn_exp2f(fmaf(s[m][2 * e], scale_log2e, -m_scaled[m]));
+                    const float w = __builtin_amdgcn_exp2f(fmaf(s[m][2 * e + 1], scale_log2e, -m_scaled[m]));
+                    sum[m] += v + w;
+                    uint32_t pw = __builtin_bit_cast(uint32_t, bf16x2_t{(__bf16)v, (__bf16)w});      // at most 256: half a step of bf16, as every operand of the products
+                    asm volatile("" : "+v"(pw));
+                    p[m][e >> 2][e & 3] = pw;
                 }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -213,57 +218,60 @@ __global__ __launch_bounds__(64 * PackedCfg<HD>::NW, PackedCfg<HD>::NW / 4) void
             if (i + PF < NV) vread(i + PF);
 #pragma unroll
             for (int m = 0; m < MQ; ++m)
-                oacc[m][i % C::NMT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i], p[m][i / C::NMT], oacc[m][i % C::NMT], 0, 0, 0);
+                oacc[m][i % C::NMT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i], __builtin_bit_cast(bf16x8_t, p[m][i / C::NMT]), oacc[m][i % C::NMT], 0, 0, 0);
 #pragma unroll
             for (int m = 0; m < MQ; ++m)
+                if (next) {
 #pragma unroll
-                for (int e = 16 * i / NV; e < 16 * (i + 1) / NV; ++e) mx[m] = fmaxf(mx[m], s_next[m][e]);
+                    for (int e = 16 * i / NV; e < 16 * (i + 1) / NV; ++e) mx[m] = fmaxf(mx[m], s_next[m][e]);
+                    asm volatile("" : "+v"(mx[m]));
+                }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
     constexpr int HALF = 32 * C::ROWB;
-    // Tile kt, the scores of whose first half are there: the second half's beside it, then the next tile's (of whatever the stage
-    // holds behind the last one: not used).
-    auto body = [&](int cur, int next, int key0, bool mask) __attribute__((always_inline)) {
+    // A tile, the scores of whose first half are there; the second half's come beside its softmax.  (To take the next
+    // tile's first scores beside the second half as well needs a third stage: one work-group of eight waves per CU instead of
+    // two of four, 333 us for the 274 of 64/8 heads of 128 over 3333 + 130 + 1 + 1777 tokens.)
+    auto body = [&](int cur, int key0, bool mask) __attribute__((always_inline)) {
         settle(sa, key0, mask);
-        step(sa, cur + C::TILE_BYTES, sb, cur + HALF);
+        step(sa, cur + C::TILE_BYTES, sb, cur + HALF, true);
         settle(sb, key0 + 32, mask);
-        step(sb, cur + C::TILE_BYTES + HALF, sa, next);
+        step(sb, cur + C::TILE_BYTES + HALF, sa, 0, false);
     };
-    int st0 = 0, st1 = 1, st2 = 2;           // stages of the tiles kt, kt + 1, kt + 2
     auto enter = [&](int kt) __attribute__((always_inline)) {
-        // tiles kt and kt + 1 have landed, this wave's part by the wait, everybody's by the barrier; and everybody is
-        // done with tile kt - 1, whose stage tile kt + 2 takes
+        // tile kt has landed, this wave's part by the wait, everybody's by the barrier; and everybody is done with tile kt - 1,
+        // whose stage tile kt + 1 takes
         __builtin_amdgcn_s_waitcnt(sp_waitcnt(0, 15));
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (kt + 2 < ntiles) issue(kt + 2, st2);
+        if (kt + 1 < ntiles) issue(kt + 1, (kt + 1) & 1);
     };
-    auto rotate = [&] { const int t = st0; st0 = st1; st1 = st2; st2 = t; };
     issue(0, 0);
-    if (ntiles > 1) issue(1, 1);
     // One barrier per tile for every wave, whatever it has to do in it.  The diagonal and a ragged end lie in a wave's last
     // tile: it alone is masked, outside the loop.
     int kt = 0;
     enter(0);
     if (mine > 0) {
-        scores(0, sa);
+        auto begin = [&]() __attribute__((always_inline)) {
+            scores((kt & 1) * C::STAGE, sa);
 #pragma unroll
-        for (int m = 0; m < MQ; ++m) {
-            mx[m] = sa[m][0];
+            for (int m = 0; m < MQ; ++m) {
+                mx[m] = sa[m][0];
 #pragma unroll
-            for (int e = 1; e < 16; ++e) mx[m] = fmaxf(mx[m], sa[m][e]);
-        }
+                for (int e = 1; e < 16; ++e) mx[m] = fmaxf(mx[m], sa[m][e]);
+            }
+        };
+        begin();
         for (; kt + 1 < mine;) {
-            body(st0 * C::STAGE, st1 * C::STAGE, kt * KB, false);
-            rotate();
+            body((kt & 1) * C::STAGE, kt * KB, false);
             enter(++kt);
+            begin();
         }
-        body(st0 * C::STAGE, st1 * C::STAGE, kt * KB, true);
+        body((kt & 1) * C::STAGE, kt * KB, true);
     }
     while (kt + 1 < ntiles) {
-        rotate();
         enter(++kt);
     }
 #pragma unroll
@@ -287,25 +295,30 @@ __global__ __launch_bounds__(64 * PackedCfg<HD>::NW, PackedCfg<HD>::NW / 4) void
     }
 }
 
-template <int HD>
+template <int HD, int NW>
 hipError_t launch_packed(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* lse, const PackedShape& a) {
-    typedef PackedCfg<HD> G;
+    typedef PackedCfg<HD, NW> G;
     static LdsLimitOnce lds_limit;
-    hipError_t e = lds_limit.set(reinterpret_cast<const void*>(attn_packed_kernel<HD>), G::LDS);
+    hipError_t e = lds_limit.set(reinterpret_cast<const void*>(attn_packed_kernel<HD, NW>), G::LDS);
     if (e != hipSuccess) return e;
     const int slots = a.T / G::QB + a.n;
-    attn_packed_kernel<HD><<<dim3((unsigned)((long)slots * a.Hq)), 64 * G::NW, G::LDS, st>>>(qkv, a.cu, o, lse, a.n, a.T, a.Hq, a.Hkv,
+    attn_packed_kernel<HD, NW><<<dim3((unsigned)((long)slots * a.Hq)), 64 * G::NW, G::LDS, st>>>(qkv, a.cu, o, lse, a.n, a.T, a.Hq, a.Hkv,
                                                                                              a.causal, 1.4426950408889634f / sqrtf((float)HD));
     return hipGetLastError();
+}
+
+template <int HD>
+hipError_t launch_hd(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* lse, const PackedShape& a) {
+    return launch_packed<HD, 4>(st, qkv, o, lse, a);
 }
 
 }  // namespace
 
 hipError_t spk_launch_attention_packed(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* lse, const PackedShape& a) {
     switch (a.hd) {
-        case 64: return launch_packed<64>(st, qkv, o, lse, a);
-        case 80: return launch_packed<80>(st, qkv, o, lse, a);
-        case 128: return launch_packed<128>(st, qkv, o, lse, a);
+        case 64: return launch_hd<64>(st, qkv, o, lse, a);
+        case 80: return launch_hd<80>(st, qkv, o, lse, a);
+        case 128: return launch_hd<128>(st, qkv, o, lse, a);
         default: return hipErrorInvalidValue;
     }
 }
