@@ -23,42 +23,9 @@
 // SIMD at head_dim 128), dq and dk/dv together with rowsum(dO * O), us: 8 x 2048, 32 heads of 128, causal
 // 2062 -> 1388; 8 x 1024, 16 heads of 128 399 -> 280; 4 x 1024, 64 query and 8 key heads of 128 748 -> 463;
 // 5 x 777, 32 and 8 heads of 64 231 -> 121; 32 x 257, 16 heads of 80, bidirectional 160 -> 145.
-#include "sp_gemm.h"
-#include "sp_packed.h"
+#include "sp_attn.h"
 
 namespace {
-
-// A 64-row token tile in LDS: rows of ROWB bytes (head_dim 80: 192, the padding is never loaded), the 16-byte
-// chunk c of row r at position c ^ swz(r).  swz serves both readers: the 16 rows of a straight 16-byte read
-// fall on all banks, and the four consecutive rows of a transposing read in different 64-byte blocks.  It has
-// period 16 in r, and r + 8 flips exactly bit 1 (the hi half of a transposed fragment: address ^ 32).
-template <int HD>
-struct TokTile {
-    static constexpr int ROWB = HD == 80 ? 192 : HD * 2, CPR = HD / 8;
-    static constexpr int NKS = HD / 16, NMT = (HD + 31) / 32;
-    static constexpr int ROWS = 64, BYTES = ROWS * ROWB;
-    __device__ static int swz(int r) {
-        return HD == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : HD == 64 ? (((r >> 1) & 1) << 2) | ((r >> 2) & 3) : (r >> 2) & 3;
-    }
-    // lane part of the straight fragment of k-step ks: row l32, head-dimension elements 16 ks + 8 half ..
-    __device__ static int row_pos(int ks, int l32, int half) { return l32 * ROWB + (((2 * ks + half) ^ swz(l32)) << 4); }
-    __device__ static bf16x8_t row_frag(const unsigned char* p) { return *reinterpret_cast<const bf16x8_t*>(p); }
-    // Transposed MFMA operand: the lane ends up with head-dimension row (lane & 31) of the 32-row block mt and
-    // the eight tokens 4*half + {0..3} and 8 + 4*half + {0..3} of a 16-token step -- the token order in which
-    // the score tiles hold their bf16 operands.  ds_read_b64_tr_b16 works on groups of 16 lanes: lane s
-    // supplies the address of four values of one token row, lane i receives element i%4 of the blocks
-    // supplied by lanes i/4, i/4+4, i/4+8, i/4+12.
-    __device__ static int tr_pos(int mt, int lane) {
-        const int s16 = lane & 15, row = 4 * (lane >> 5) + (s16 >> 2);
-        const int chunk = mt * 4 + 2 * ((lane >> 4) & 1) + ((s16 & 3) >> 1);
-        return row * ROWB + ((chunk ^ swz(row)) << 4) + (s16 & 1) * 8;
-    }
-    __device__ static bf16x8_t tr_frag(const unsigned char* step, int pos) {
-        const s16x4_t lo = sp_tr_read((lds_s16x4_ptr)(step + pos));
-        const s16x4_t hi = sp_tr_read((lds_s16x4_ptr)(step + (pos ^ 32) + 8 * ROWB));
-        return __builtin_bit_cast(bf16x8_t, s16x8_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
-    }
-};
 
 // Loads of one stage: two token tiles (X, then Y) of the same rows, NW waves.  Instruction i of a wave lands at
 // byte (wave * NI + i) * 1024 + lane * 16 of the stage.
@@ -117,12 +84,10 @@ __device__ __forceinline__ f32x16_t zero16() {
 // A work-group owns 128 queries of one head (a wave 32 of them, one query per lane as the B
 // operand) and walks 64-key tiles: S^T = K Q^T and dP^T = V dO^T read the tiles straight,
 // dQ^T += K^T dS^T reads K through the transposing LDS read.
-// PACKED: the sequences of sp_packed.h (S = rows of the buffers; lse and delta [Hq][S]), a slot per 128 rows.
-template <int HD, bool PACKED>
+template <int HD>
 __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dO,
                                                           const float* __restrict__ lse, const float* __restrict__ delta,
-                                                          bf16_t* __restrict__ dqkv, const int* __restrict__ cu, int n_seqs,
-                                                          int S, int Hq, int Hkv, int ld_qkv,
+                                                          bf16_t* __restrict__ dqkv, int S, int Hq, int Hkv, int ld_qkv,
                                                           int causal, float scale, float scale_log2e) {
     typedef TokTile<HD> T;
     typedef StageLoad<HD, 4> Load;
@@ -137,18 +102,10 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(const bf16_t* __res
     const int job = xcd_remap(blockIdx.x + (int)gridDim.x * (blockIdx.y + (int)gridDim.y * blockIdx.z),
                               (int)(gridDim.x * gridDim.y * gridDim.z));
     const int bx = job % (int)gridDim.x, h = (job / (int)gridDim.x) % (int)gridDim.y, b = job / (int)(gridDim.x * gridDim.y);
-    int qb = causal ? gridDim.x - 1 - bx : bx;
-    size_t tok0 = (size_t)b * S, row0 = ((size_t)b * Hq + h) * S;       // row0: of lse and delta
-    if (PACKED) {
-        const PackedBlock p = packed_block<128>(cu, n_seqs, S, bx);
-        if (p.blk * 128 >= p.len) return;
-        qb = p.blk;
-        tok0 = p.row0;
-        row0 = (size_t)h * S + p.row0;
-        S = p.len;
-    }
+    const int qb = causal ? gridDim.x - 1 - bx : bx;
     const int kvh = h / (Hq / Hkv);
     const int q0 = qb * 128, wq0 = q0 + wave * 32, qi = wq0 + l32;
+    const size_t tok0 = (size_t)b * S;
     const int qr = min(qi, S - 1);
     const bf16_t* kbase = qkv + tok0 * ld_qkv + (size_t)Hq * HD + (size_t)kvh * HD;
     const bf16_t* vbase = kbase + (size_t)Hkv * HD;
@@ -168,8 +125,8 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(const bf16_t* __res
             dof[ks] = *reinterpret_cast<const bf16x8_t*>(dp + ks * 16);
         }
     }
-    const float lse_q = lse[row0 + qr] * 1.4426950408889634f;
-    const float delta_q = delta[row0 + qr];
+    const float lse_q = lse[((size_t)b * Hq + h) * S + qr] * 1.4426950408889634f;
+    const float delta_q = delta[((size_t)b * Hq + h) * S + qr];
     int kpos[T::NKS], tpos[T::NMT];
 #pragma unroll
     for (int ks = 0; ks < T::NKS; ++ks) kpos[ks] = T::row_pos(ks, l32, half);
@@ -251,11 +208,10 @@ struct DkvCfg {
     static_assert(4 * TokTile<HD>::NMT * 16 * 256 <= 2 * StageLoad<HD, 8>::STAGE, "one accumulator set of four waves fits the stages");
 };
 
-template <int HD, bool PACKED>
+template <int HD>
 __global__ __launch_bounds__(512) void attn_bwd_dkv_kernel(const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dO,
                                                            const float* __restrict__ lse, const float* __restrict__ delta,
-                                                           bf16_t* __restrict__ dqkv, const int* __restrict__ cu, int n_seqs,
-                                                           int S, int Hq, int Hkv,
+                                                           bf16_t* __restrict__ dqkv, int S, int Hq, int Hkv,
                                                            int ld_qkv, int causal, float scale, float scale_log2e) {
     typedef TokTile<HD> T;
     typedef StageLoad<HD, 8> Load;
@@ -270,19 +226,10 @@ __global__ __launch_bounds__(512) void attn_bwd_dkv_kernel(const bf16_t* __restr
     // the same XCD-contiguous order as in the dq kernel: the key blocks of a head share its queries
     const int job = xcd_remap(blockIdx.x + (int)gridDim.x * (blockIdx.y + (int)gridDim.y * blockIdx.z),
                               (int)(gridDim.x * gridDim.y * gridDim.z));
-    int bx = job % (int)gridDim.x;
-    const int kvh = (job / (int)gridDim.x) % (int)gridDim.y, b = job / (int)(gridDim.x * gridDim.y);
+    const int bx = job % (int)gridDim.x, kvh = (job / (int)gridDim.x) % (int)gridDim.y, b = job / (int)(gridDim.x * gridDim.y);
     const int grp = Hq / Hkv;
-    size_t tok0 = (size_t)b * S, row0 = (size_t)b * Hq * S, ld_row = S;      // row0, ld_row: of lse and delta
-    if (PACKED) {
-        const PackedBlock p = packed_block<128>(cu, n_seqs, S, bx);
-        if (p.blk * 128 >= p.len) return;
-        // the first key block has the most queries under a causal mask
-        bx = causal ? (p.len - 1) / 128 - p.blk : p.blk;
-        tok0 = row0 = p.row0;
-        S = p.len;
-    }
     const int k0 = bx * 128, wk0 = k0 + kg * 32, kj = wk0 + l32;
+    const size_t tok0 = (size_t)b * S;
     const int ld_do = Hq * HD;
     const bf16_t* kbase = qkv + tok0 * ld_qkv + (size_t)Hq * HD + (size_t)kvh * HD;
     const bf16_t* vbase = kbase + (size_t)Hkv * HD;
@@ -299,7 +246,7 @@ __global__ __launch_bounds__(512) void attn_bwd_dkv_kernel(const bf16_t* __restr
         const int q0 = q_begin + (tile % tiles_per_head) * QT;
         ld.issue(smem + (tile & 1) * Load::STAGE, wave, qkv + tok0 * ld_qkv + h * HD, ld_qkv, dO + tok0 * ld_do + h * HD, ld_do, q0, S - 1, S - 1);
         if (threadIdx.x < QT) {
-            const size_t row = row0 + h * ld_row + min(q0 + (int)threadIdx.x, S - 1);
+            const size_t row = ((size_t)b * Hq + h) * S + min(q0 + (int)threadIdx.x, S - 1);
             r_lse = lse[row] * 1.4426950408889634f;
             r_delta = delta[row];
         }
@@ -414,24 +361,22 @@ __global__ __launch_bounds__(512) void attn_bwd_dkv_kernel(const bf16_t* __restr
     if (sub == 1) take_and_store(dv, Hkv, 1.0f);
 }
 
-// B sequences of S rows, or (cu != nullptr) n_seqs packed ones in S rows.
-template <int HD, bool PACKED>
-hipError_t launch_bwd(hipStream_t st, const AttnBwdArgs& g, const AttnShape& a, const int* cu, int n_seqs) {
+template <int HD>
+hipError_t launch_bwd(hipStream_t st, const AttnBwdArgs& g, const AttnShape& a) {
     constexpr int LDS_Q = 2 * StageLoad<HD, 4>::STAGE, LDS_KV = DkvCfg<HD>::LDS;
     static LdsLimitOnce lim_q, lim_kv;
-    hipError_t e = lim_q.set(reinterpret_cast<const void*>(attn_bwd_dq_kernel<HD, PACKED>), LDS_Q);
-    if (e == hipSuccess) e = lim_kv.set(reinterpret_cast<const void*>(attn_bwd_dkv_kernel<HD, PACKED>), LDS_KV);
+    hipError_t e = lim_q.set(reinterpret_cast<const void*>(attn_bwd_dq_kernel<HD>), LDS_Q);
+    if (e == hipSuccess) e = lim_kv.set(reinterpret_cast<const void*>(attn_bwd_dkv_kernel<HD>), LDS_KV);
     if (e != hipSuccess) return e;
     const float scale = 1.0f / sqrtf((float)a.hd), sl2 = scale * 1.4426950408889634f;
-    const int blocks = PACKED ? a.S / 128 + n_seqs : (a.S + 127) / 128;
-    dim3 gq(blocks, a.Hq, a.B);
-    attn_bwd_dq_kernel<HD, PACKED><<<gq, 256, LDS_Q, st>>>(g.qkv, g.dO, g.lse, g.delta, g.dqkv, cu, n_seqs, a.S, a.Hq, a.Hkv, a.ld_qkv,
-                                                           a.causal, scale, sl2);
+    dim3 gq((a.S + 127) / 128, a.Hq, a.B);
+    attn_bwd_dq_kernel<HD><<<gq, 256, LDS_Q, st>>>(g.qkv, g.dO, g.lse, g.delta, g.dqkv, a.S, a.Hq, a.Hkv, a.ld_qkv, a.causal,
+                                                   scale, sl2);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    dim3 gk(blocks, a.Hkv, a.B);
-    attn_bwd_dkv_kernel<HD, PACKED><<<gk, 512, LDS_KV, st>>>(g.qkv, g.dO, g.lse, g.delta, g.dqkv, cu, n_seqs, a.S, a.Hq, a.Hkv, a.ld_qkv,
-                                                             a.causal, scale, sl2);
+    dim3 gk((a.S + 127) / 128, a.Hkv, a.B);
+    attn_bwd_dkv_kernel<HD><<<gk, 512, LDS_KV, st>>>(g.qkv, g.dO, g.lse, g.delta, g.dqkv, a.S, a.Hq, a.Hkv, a.ld_qkv,
+                                                     a.causal, scale, sl2);
     return hipGetLastError();
 }
 
@@ -442,19 +387,9 @@ hipError_t spk_launch_attention_bwd(hipStream_t st, const AttnBwdArgs& g, const 
     if (a.Hkv <= 0 || a.Hq % a.Hkv || a.ld_qkv % 8 || a.B > 65535 || a.Hq > 65535) return hipErrorInvalidValue;
     if (!g.qkv || !g.dO || !g.lse || !g.delta || !g.dqkv) return hipErrorInvalidValue;
     switch (a.hd) {
-        case 64: return launch_bwd<64, false>(st, g, a, nullptr, 0);
-        case 80: return launch_bwd<80, false>(st, g, a, nullptr, 0);
-        case 128: return launch_bwd<128, false>(st, g, a, nullptr, 0);
-    }
-    return hipErrorInvalidValue;
-}
-
-hipError_t spk_launch_attention_packed_bwd(hipStream_t st, const AttnBwdArgs& g, const PackedShape& a) {
-    const AttnShape s{1, a.T, a.Hq, a.Hkv, a.hd, a.causal, (a.Hq + 2 * a.Hkv) * a.hd};
-    switch (a.hd) {
-        case 64: return launch_bwd<64, true>(st, g, s, a.cu, a.n);
-        case 80: return launch_bwd<80, true>(st, g, s, a.cu, a.n);
-        case 128: return launch_bwd<128, true>(st, g, s, a.cu, a.n);
+        case 64: return launch_bwd<64>(st, g, a);
+        case 80: return launch_bwd<80>(st, g, a);
+        case 128: return launch_bwd<128>(st, g, a);
     }
     return hipErrorInvalidValue;
 }

@@ -1,0 +1,555 @@
+// Backward of the attention over packed prompts: dq, dk, dv from q, k, v, dO, the forward's log-sum-exp and
+// delta = rowsum(dO * O), without atomics, in one launch of two kinds of work-groups that do not depend on one another:
+//   dk/dv -- a work-group owns 32 KG keys of one key/value head and walks the queries of every query head that shares it;
+//   dq    -- a work-group owns 256 queries of one head, or 128 of two heads that share keys and values, and walks the keys.
+// P = exp(s - lse), dS = P (dP - delta), dP = dO V^T; layouts and tiles are those of k_attn_bwd.hip.
+//
+// What bounds it: 7 products of 2 hd flops per pair of a query and a key on the matrix pipe, 1 KB of LDS per MFMA of 32
+// cycles (which four SIMDs drawing at once would all but use up), and the arithmetic of P and dS on the vector pipe.  Every
+// wave therefore reads its fragments a few MFMAs ahead, in an order that the source fixes, and works P beside the MFMAs
+// of dP, and dS beside those of dV (dk/dv) or of the next 32 keys' scores (dq).  One launch: a short batch has too few
+// blocks of either kind to fill the chip.
+#include <stdlib.h>
+#include "sp_attn.h"
+#include "sp_packed.h"
+
+namespace {
+
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ bf16x8_t lds_b128(const unsigned char* __restrict__ p) { return *reinterpret_cast<const bf16x8_t*>(p); }
+__device__ __forceinline__ float4 lds_f4(const float* __restrict__ p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ uint32_t pack2(float a, float b) { return __builtin_bit_cast(uint32_t, bf16x2_t{(__bf16)a, (__bf16)b}); }
+
+constexpr int BWD_WAVES = 8;
+// The one of n steps that share out `total` items evenly which takes item e.
+constexpr int step_of(int e, int n, int total) {
+    int i = 0;
+    while (e >= total * (i + 1) / n) ++i;
+    return i;
+}
+constexpr float LOG2E = 1.4426950408889634f;
+
+// Fragment addresses of a token tile (TokTile): the lane's part, the k-step or 32-row block on top.
+template <int HD>
+struct FragAt {
+    typedef TokTile<HD> T;
+    int r0, r1, t0;
+    __device__ void init(int lane) {
+        r0 = T::row_pos(0, lane & 31, lane >> 5);
+        r1 = T::row_pos(1, lane & 31, lane >> 5);
+        t0 = T::tr_pos(0, lane);
+    }
+    // rows of 128 and 256 bytes: an exclusive or; of 192: two k-steps of four chunks, or a block, are an offset
+    __device__ bf16x8_t row(const unsigned char* smem, int base, int ks) const {
+        return lds_b128(smem + (HD != 80 ? (base + r0) ^ (ks << 5) : base + ((ks & 1) ? r1 : r0) + (ks >> 1) * 64));
+    }
+    __device__ bf16x8_t tr(const unsigned char* smem, int base, int mt) const {
+        const int a = HD != 80 ? (base + t0) ^ (mt << 6) : base + t0 + mt * 64;
+        const s16x4_t lo = sp_tr_read((lds_s16x4_ptr)(smem + a));
+        const s16x4_t hi = sp_tr_read((lds_s16x4_ptr)(smem + (a ^ 32) + 8 * T::ROWB));
+        return __builtin_bit_cast(bf16x8_t, s16x8_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+    }
+};
+
+// Loads of a tile of ROWS token rows by eight waves, straight into LDS.  Rows past those that exist and the padding of
+// 192-byte rows lie outside the buffer that the load is given and land as zeros.
+template <int HD, int ROWS>
+struct TileLoad {
+    typedef TokTile<HD> T;
+    static constexpr int BYTES = ROWS * T::ROWB, NINST = BYTES / 1024, NI = (NINST + BWD_WAVES - 1) / BWD_WAVES;
+    static_assert(BYTES % 1024 == 0, "whole load instructions");
+    int row[NI], col[NI];
+    __device__ void init(int wave, int lane) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const int off = (wave * NI + i) * 1024 + lane * 16;
+            row[i] = off / T::ROWB;
+            const int c = ((off % T::ROWB) >> 4) ^ T::swz(row[i]);
+            col[i] = c < T::CPR ? c * 16 : -1;
+        }
+    }
+    __device__ __forceinline__ void issue(unsigned char* dst, int wave, const bf16_t* src, int ld, int rows) const {
+#if defined(__HIP_DEVICE_COMPILE__)
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(src), 0, min(rows, ROWS) * ld * 2, 0x00020000);
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+            if (NINST % BWD_WAVES == 0 || wave * NI + i < NINST)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void_ptr)(dst + (wave * NI + i) * 1024), 16,
+                                                         col[i] < 0 ? -1 : row[i] * ld * 2 + col[i], 0, 0, 0);
+#endif
+    }
+};
+
+__device__ __forceinline__ void landed() {
+    // this wave's loads and LDS accesses; behind the barrier every wave's
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(sp_waitcnt(0, 0));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+__device__ __forceinline__ f32x16_t zeros() {
+    f32x16_t z;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) z[e] = 0.f;
+    return z;
+}
+
+struct BwdDev {
+    const bf16_t *qkv, *dO;
+    const float *lse, *delta;
+    bf16_t* dqkv;
+    const int* cu;
+    int n, T, Hq, Hkv, causal;
+    float scale, scale_log2e;
+};
+
+__device__ __forceinline__ int near_heads(int i, int heads) { return heads & 7 ? i : (i & 7) * (heads >> 3) + (i >> 3); }
+
+// -------------------------------------------------------------------------------------------------- dq
+template <int HD>
+struct DqCfg {
+    typedef TokTile<HD> T;
+    static constexpr int STAGE = 2 * T::BYTES, LDS = 2 * STAGE;      // {K, V} of 64 keys
+};
+
+template <int HD>
+__device__ __forceinline__ void dq_group(const BwdDev& g, unsigned char* smem, int id) {
+    typedef TokTile<HD> T;
+    typedef DqCfg<HD> C;
+    constexpr int KEYS = T::ROWS, NK = T::NKS, NV = 2 * T::NMT, PF = 3;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l32 = lane & 31, half = lane >> 5;
+    const int Hq = g.Hq, Hkv = g.Hkv, grp = Hq / Hkv, ld = (Hq + 2 * Hkv) * HD;
+    const bool two = grp % 2 == 0;                    // two heads of 128 queries
+    const int units = two ? Hq / 2 : Hq, slot = id / units, unit = near_heads(id - slot * units, units);
+    const int h = two ? unit * 2 + (wave >> 2) : unit;
+    const PackedBlock pb = two ? packed_block<128>(g.cu, g.n, g.T, slot) : packed_block<256>(g.cu, g.n, g.T, slot);
+    const int rows = two ? 128 : 256, q0 = pb.blk * rows, len = pb.len;
+    if (q0 >= len) return;
+    const int wq0 = q0 + (two ? wave & 3 : wave) * 32, qi = wq0 + l32;
+    const size_t tok0 = pb.row0, row0 = (size_t)h * g.T + tok0;
+    const int qr = min(qi, len - 1);
+    const bf16_t* kbase = g.qkv + tok0 * ld + (size_t)(Hq + h / grp) * HD;
+    const bf16_t* vbase = kbase + (size_t)Hkv * HD;
+    const int ntiles = ((g.causal ? min(len, q0 + rows) : len) + KEYS - 1) / KEYS;
+    const int mine = wq0 >= len ? 0 : ((g.causal ? min(len, wq0 + 32) : len) + KEYS - 1) / KEYS;
+    TileLoad<HD, KEYS> tl;
+    tl.init(wave, lane);
+    auto issue = [&](int t) __attribute__((always_inline)) {
+        unsigned char* st = smem + (t & 1) * C::STAGE;
+        tl.issue(st, wave, kbase + (size_t)t * KEYS * ld, ld, len - t * KEYS);
+        tl.issue(st + T::BYTES, wave, vbase + (size_t)t * KEYS * ld, ld, len - t * KEYS);
+    };
+    issue(0);
+    bf16x8_t qf[NK], dof[NK];
+    {
+        const bf16_t* qp = g.qkv + (tok0 + qr) * ld + h * HD + half * 8;
+        const bf16_t* dp = g.dO + (tok0 + qr) * (size_t)(Hq * HD) + h * HD + half * 8;
+#pragma unroll
+        for (int ks = 0; ks < NK; ++ks) {
+            qf[ks] = *reinterpret_cast<const bf16x8_t*>(qp + ks * 16);
+            dof[ks] = *reinterpret_cast<const bf16x8_t*>(dp + ks * 16);
+        }
+    }
+    const float lse_q = g.lse[row0 + qr] * LOG2E, delta_q = g.delta[row0 + qr];
+    FragAt<HD> at;
+    at.init(lane);
+    f32x16_t acc[T::NMT];
+#pragma unroll
+    for (int t = 0; t < T::NMT; ++t) acc[t] = zeros();
+
+    auto mask_scores = [&](f32x16_t& s, int key0) __attribute__((always_inline)) {
+        const int last = min(len - 1, g.causal ? qi : len - 1) - key0 - 4 * half;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = (e >> 2) * 8 + (e & 3) <= last ? s[e] : -INFINITY;
+    };
+    // 32 keys: dP beside P (which takes the place of the scores), from the V rows at base_v
+    auto probs = [&](f32x16_t& s, f32x16_t& dp, int base_v) __attribute__((always_inline)) {
+        bf16x8_t vf[NK];
+#pragma unroll
+        for (int i = 0; i < PF; ++i) vf[i] = at.row(smem, base_v, i);
+        dp = zeros();
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < NK; ++i) {
+            if (i + PF < NK) vf[i + PF] = at.row(smem, base_v, i + PF);
+            dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i], dof[i], dp, 0, 0, 0);
+#pragma unroll
+            for (int e = 16 * i / NK; e < 16 * (i + 1) / NK; ++e) {
+                float p = __builtin_amdgcn_exp2f(fmaf(s[e], g.scale_log2e, -lse_q));
+                asm volatile("" : "+v"(p));
+                s[e] = p;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // dS of 32 keys (P in s) beside the next scores, if any, from the K rows at base_k
+    auto grads = [&](const f32x16_t& s, const f32x16_t& dp, u32x4_t (&ds)[2], f32x16_t& s_next, int base_k, bool next) __attribute__((always_inline)) {
+        bf16x8_t kf[NK];
+        if (next) {
+#pragma unroll
+            for (int i = 0; i < PF; ++i) kf[i] = at.row(smem, base_k, i);
+            s_next = zeros();
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < NK; ++i) {
+            if (next) {
+                if (i + PF < NK) kf[i + PF] = at.row(smem, base_k, i + PF);
+                s_next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[i], s_next, 0, 0, 0);
+            }
+#pragma unroll
+            for (int e = 8 * i / NK; e < 8 * (i + 1) / NK; ++e) {
+                uint32_t w = pack2(s[2 * e] * (dp[2 * e] - delta_q), s[2 * e + 1] * (dp[2 * e + 1] - delta_q));
+                asm volatile("" : "+v"(w));
+                ds[e >> 2][e & 3] = w;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto output = [&](const u32x4_t (&ds)[2], int base) __attribute__((always_inline)) {
+        bf16x8_t tf[NV];
+        auto read = [&](int i) __attribute__((always_inline)) { tf[i] = at.tr(smem, base + 16 * (i / T::NMT) * T::ROWB, i % T::NMT); };
+#pragma unroll
+        for (int i = 0; i < PF; ++i) read(i);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (i + PF < NV) read(i + PF);
+            acc[i % T::NMT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tf[i], __builtin_bit_cast(bf16x8_t, ds[i / T::NMT]), acc[i % T::NMT], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto tile = [&](int t, bool mask) __attribute__((always_inline)) {
+        constexpr int HALF = 32 * T::ROWB;
+        const int k = (t & 1) * C::STAGE, v = k + T::BYTES;
+        f32x16_t sa, sb, dp;
+        u32x4_t ds[2];
+        {
+            bf16x8_t kf[NK];
+#pragma unroll
+            for (int i = 0; i < PF; ++i) kf[i] = at.row(smem, k, i);
+            sa = zeros();
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < NK; ++i) {
+                if (i + PF < NK) kf[i + PF] = at.row(smem, k, i + PF);
+                sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[i], sa, 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        if (mask) mask_scores(sa, t * KEYS);
+        probs(sa, dp, v);
+        grads(sa, dp, ds, sb, k + HALF, true);
+        output(ds, k);
+        if (mask) mask_scores(sb, t * KEYS + 32);
+        probs(sb, dp, v + HALF);
+        grads(sb, dp, ds, sa, 0, false);
+        output(ds, k + HALF);
+    };
+    // one barrier per tile for every wave; the diagonal and a ragged end lie in a wave's last tile
+    int t = 0;
+    auto enter = [&]() __attribute__((always_inline)) {
+        landed();
+        if (t + 1 < ntiles) issue(t + 1);
+    };
+    enter();
+    if (mine > 0) {
+        while (t + 1 < mine) {
+            tile(t, false);
+            ++t;
+            enter();
+        }
+        tile(t, true);
+    }
+    while (t + 1 < ntiles) {
+        ++t;
+        enter();
+    }
+    if (qi < len) {
+        bf16_t* op = g.dqkv + (tok0 + qi) * ld + h * HD;
+#pragma unroll
+        for (int mt = 0; mt < T::NMT; ++mt)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int e0 = mt * 32 + k * 8 + half * 4;
+                if (e0 < HD)
+                    *reinterpret_cast<uint2*>(op + e0) = make_uint2(pack2(acc[mt][k * 4] * g.scale, acc[mt][k * 4 + 1] * g.scale),
+                                                                    pack2(acc[mt][k * 4 + 2] * g.scale, acc[mt][k * 4 + 3] * g.scale));
+            }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- dk, dv
+// Wave w takes the 32 keys of group w % KG (one key per lane as the B operand of S = Q K^T and dP = dO V^T) against the 32
+// queries of part w / KG of each tile; the parts' sums are added through LDS at the end.
+template <int HD, int KG>
+struct DkvCfg {
+    typedef TokTile<HD> T;
+    static constexpr int SUBS = BWD_WAVES / KG, ROWS = 32 * SUBS, KEYS = 32 * KG;
+    static constexpr bool K_IN_LDS = HD == 128;       // K fragments would not fit beside the accumulators
+    static constexpr int TILE = ROWS * T::ROWB, STAGE = 2 * TILE;
+    static constexpr int KBYTES = K_IN_LDS ? KEYS * T::ROWB : 0;
+    static constexpr int LDS = 2 * STAGE + KBYTES + 2 * 2 * ROWS * 4;
+    static_assert((SUBS - 1) * KG * T::NMT * 16 * 256 <= 2 * STAGE, "the parts' sums fit the stages");
+    static_assert(LDS <= 160 * 1024, "fits the LDS");
+};
+
+template <int HD, int KG>
+__device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, int id) {
+    typedef TokTile<HD> T;
+    typedef DkvCfg<HD, KG> C;
+    constexpr int NK = T::NKS, NV = 2 * T::NMT, PF = 2;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l32 = lane & 31, half = lane >> 5, kg = wave % KG, sub = wave / KG;
+    const int Hq = g.Hq, Hkv = g.Hkv, grp = Hq / Hkv, ld = (Hq + 2 * Hkv) * HD, ld_do = Hq * HD;
+    const int slot = id / Hkv, kvh = near_heads(id - slot * Hkv, Hkv);
+    const PackedBlock pb = packed_block<C::KEYS>(g.cu, g.n, g.T, slot);
+    const int len = pb.len;
+    if (pb.blk * C::KEYS >= len) return;
+    // under a causal mask the first block has the most queries
+    const int blk = g.causal ? (len - 1) / C::KEYS - pb.blk : pb.blk;
+    const int k0 = blk * C::KEYS, wk0 = k0 + kg * 32, kj = wk0 + l32;
+    const size_t tok0 = pb.row0;
+    const bf16_t* kbase = g.qkv + tok0 * ld + (size_t)(Hq + kvh) * HD;
+    const bf16_t* vbase = kbase + (size_t)Hkv * HD;
+    unsigned char* sKeys = smem + 2 * C::STAGE;
+    float* rowvals = reinterpret_cast<float*>(smem + 2 * C::STAGE + C::KBYTES);       // [stage][lse | delta][ROWS]
+
+    // the tiles in walking order: (query head of the group, ROWS queries)
+    const int q_begin = g.causal ? k0 / C::ROWS * C::ROWS : 0;
+    const int per_head = (len - q_begin + C::ROWS - 1) / C::ROWS, n_tiles = grp * per_head;
+    TileLoad<HD, C::ROWS> tl;
+    tl.init(wave, lane);
+    float r_lse = 0.f, r_delta = 0.f;
+    int f_head = 0, f_q = q_begin;                    // of the tile fetched next
+    auto fetch = [&](int tile) __attribute__((always_inline)) {
+        const int h = kvh * grp + f_head;
+        unsigned char* st = smem + (tile & 1) * C::STAGE;
+        tl.issue(st, wave, g.qkv + (tok0 + f_q) * ld + (size_t)h * HD, ld, len - f_q);
+        tl.issue(st + C::TILE, wave, g.dO + (tok0 + f_q) * ld_do + (size_t)h * HD, ld_do, len - f_q);
+        if (threadIdx.x < C::ROWS) {
+            const size_t row = (size_t)h * g.T + tok0 + min(f_q + (int)threadIdx.x, len - 1);
+            r_lse = g.lse[row] * LOG2E;
+            r_delta = g.delta[row];
+        }
+        f_q += C::ROWS;
+        if (f_q >= len) { f_q = q_begin; ++f_head; }
+    };
+    auto put_rowvals = [&](int tile) __attribute__((always_inline)) {
+        if (threadIdx.x < C::ROWS) {
+            rowvals[(tile & 1) * 2 * C::ROWS + threadIdx.x] = r_lse;
+            rowvals[(tile & 1) * 2 * C::ROWS + C::ROWS + threadIdx.x] = r_delta;
+        }
+    };
+    if (C::K_IN_LDS) {
+        TileLoad<HD, C::KEYS> kl;
+        kl.init(wave, lane);
+        kl.issue(sKeys, wave, kbase + (size_t)k0 * ld, ld, len - k0);
+    }
+    fetch(0);
+    bf16x8_t kf_reg[C::K_IN_LDS ? 1 : NK], vf[NK];
+    {
+        const size_t kr = min(kj, len - 1);
+#pragma unroll
+        for (int ks = 0; ks < NK; ++ks) {
+            if (!C::K_IN_LDS) kf_reg[C::K_IN_LDS ? 0 : ks] = *reinterpret_cast<const bf16x8_t*>(kbase + kr * ld + half * 8 + ks * 16);
+            vf[ks] = *reinterpret_cast<const bf16x8_t*>(vbase + kr * ld + half * 8 + ks * 16);
+        }
+    }
+    FragAt<HD> at;
+    at.init(lane);
+    f32x16_t dk[T::NMT], dv[T::NMT];
+#pragma unroll
+    for (int t = 0; t < T::NMT; ++t) { dk[t] = zeros(); dv[t] = zeros(); }
+
+    put_rowvals(0);
+    landed();
+    int qs = q_begin + sub * 32;                      // this wave's first query of the tile
+    for (int tile = 0; tile < n_tiles; ++tile) {
+        const bool more = tile + 1 < n_tiles;
+        if (more) fetch(tile + 1);
+        const int q_at = (tile & 1) * C::STAGE + sub * 32 * T::ROWB, do_at = q_at + C::TILE;
+        const float* lrow = rowvals + (tile & 1) * 2 * C::ROWS + sub * 32 + half * 4;
+        // wave-uniform skips: every query of the part precedes this wave's keys, none exists, no key exists
+        if (!(qs >= len || wk0 >= len || (g.causal && qs + 31 < wk0))) {
+            f32x16_t s = zeros(), dp;
+            {
+                bf16x8_t qf[NK], kf[NK];
+                auto read = [&](int i) __attribute__((always_inline)) {
+                    qf[i] = at.row(smem, q_at, i);
+                    if (C::K_IN_LDS) kf[i] = at.row(sKeys, kg * 32 * T::ROWB, i);
+                };
+#pragma unroll
+                for (int i = 0; i < PF; ++i) read(i);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < NK; ++i) {
+                    if (i + PF < NK) read(i + PF);
+                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[i], C::K_IN_LDS ? kf[i] : kf_reg[C::K_IN_LDS ? 0 : i], s, 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            if ((g.causal && qs < wk0 + 31) || qs + 32 > len) {
+                // element e is query qs + 4 half + (e >> 2) * 8 + (e & 3)
+                const int first = (g.causal ? kj : 0) - qs - 4 * half, end = len - qs - 4 * half;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int q = (e >> 2) * 8 + (e & 3);
+                    s[e] = q >= first && q < end ? s[e] : -INFINITY;
+                }
+            }
+            // dP beside P, which takes the place of the scores; then dV beside dS; then dK
+            u32x4_t pw[2], ds[2];
+            {
+                bf16x8_t df[NK];
+                float4 l4[4];
+                dp = zeros();
+                l4[0] = lds_f4(lrow);                    // the others a step ahead of their use: registers are short here
+#pragma unroll
+                for (int i = 0; i < PF; ++i) df[i] = at.row(smem, do_at, i);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < NK; ++i) {
+                    if (i + PF < NK) df[i + PF] = at.row(smem, do_at, i + PF);
+#pragma unroll
+                    for (int k = 1; k < 4; ++k)
+                        if (step_of(2 * k, NK, 8) == i + 1) l4[k] = lds_f4(lrow + k * 8);
+                    dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(df[i], vf[i], dp, 0, 0, 0);
+#pragma unroll
+                    for (int e = 8 * i / NK; e < 8 * (i + 1) / NK; ++e) {
+                        const float4 l = l4[e >> 1];
+                        const float a = __builtin_amdgcn_exp2f(fmaf(s[2 * e], g.scale_log2e, -((e & 1) ? l.z : l.x)));
+                        const float b = __builtin_amdgcn_exp2f(fmaf(s[2 * e + 1], g.scale_log2e, -((e & 1) ? l.w : l.y)));
+                        uint32_t w = pack2(a, b);
+                        asm volatile("" : "+v"(w));
+                        pw[e >> 2][e & 3] = w;
+                        s[2 * e] = a;
+                        s[2 * e + 1] = b;
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            {
+                bf16x8_t tf[NV];
+                float4 d4[4];
+                auto read = [&](int i) __attribute__((always_inline)) { tf[i] = at.tr(smem, do_at + 16 * (i / T::NMT) * T::ROWB, i % T::NMT); };
+                d4[0] = lds_f4(lrow + C::ROWS);
+#pragma unroll
+                for (int i = 0; i < PF; ++i) read(i);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    if (i + PF < NV) read(i + PF);
+#pragma unroll
+                    for (int k = 1; k < 4; ++k)
+                        if (step_of(2 * k, NV, 8) == i + 1) d4[k] = lds_f4(lrow + C::ROWS + k * 8);
+                    dv[i % T::NMT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tf[i], __builtin_bit_cast(bf16x8_t, pw[i / T::NMT]), dv[i % T::NMT], 0, 0, 0);
+#pragma unroll
+                    for (int e = 8 * i / NV; e < 8 * (i + 1) / NV; ++e) {
+                        const float4 d = d4[e >> 1];
+                        uint32_t w = pack2(s[2 * e] * (dp[2 * e] - ((e & 1) ? d.z : d.x)), s[2 * e + 1] * (dp[2 * e + 1] - ((e & 1) ? d.w : d.y)));
+                        asm volatile("" : "+v"(w));
+                        ds[e >> 2][e & 3] = w;
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            {
+                bf16x8_t tf[NV];
+                auto read = [&](int i) __attribute__((always_inline)) { tf[i] = at.tr(smem, q_at + 16 * (i / T::NMT) * T::ROWB, i % T::NMT); };
+#pragma unroll
+                for (int i = 0; i < PF; ++i) read(i);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    if (i + PF < NV) read(i + PF);
+                    dk[i % T::NMT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tf[i], __builtin_bit_cast(bf16x8_t, ds[i / T::NMT]), dk[i % T::NMT], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        }
+        qs += C::ROWS;
+        if (qs - sub * 32 >= len) qs = q_begin + sub * 32;
+        if (more) put_rowvals(tile + 1);
+        landed();
+    }
+    // The parts' sums meet in the stages: dK in part 0, dV in part 1, added in the order of the parts.
+    float4* x = reinterpret_cast<float4*>(smem) + lane;
+    auto place = [&](int s, int owner) { return ((s < owner ? s : s - 1) * KG + kg) * (T::NMT * 4 * 64); };
+    auto give = [&](const f32x16_t* a, int owner) {
+        if (sub == owner) return;
+#pragma unroll
+        for (int t = 0; t < T::NMT; ++t)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                x[place(sub, owner) + (t * 4 + k) * 64] = make_float4(a[t][k * 4], a[t][k * 4 + 1], a[t][k * 4 + 2], a[t][k * 4 + 3]);
+    };
+    auto take = [&](const f32x16_t* a, int owner, int col, float f) {
+        if (sub != owner || kj >= len) return;
+        bf16_t* out = g.dqkv + (tok0 + kj) * ld + (size_t)(Hq + col + kvh) * HD;
+#pragma unroll
+        for (int t = 0; t < T::NMT; ++t)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int s = 0; s < C::SUBS; ++s) {
+                    const float4 o = s == owner ? make_float4(a[t][k * 4], a[t][k * 4 + 1], a[t][k * 4 + 2], a[t][k * 4 + 3])
+                                                : x[place(s, owner) + (t * 4 + k) * 64];
+                    v[0] += o.x; v[1] += o.y; v[2] += o.z; v[3] += o.w;
+                }
+                const int e0 = t * 32 + k * 8 + half * 4;
+                if (e0 < HD) *reinterpret_cast<uint2*>(out + e0) = make_uint2(pack2(v[0] * f, v[1] * f), pack2(v[2] * f, v[3] * f));
+            }
+    };
+    give(dk, 0);
+    sp_lds_barrier();
+    take(dk, 0, 0, g.scale);
+    sp_lds_barrier();
+    give(dv, 1);
+    sp_lds_barrier();
+    take(dv, 1, Hkv, 1.0f);
+}
+
+template <int HD, int KG>
+__global__ __launch_bounds__(BWD_WAVES * 64, 2) void attn_packed_bwd_kernel(BwdDev g, int dkv_groups) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem_bwd[];
+    if ((int)blockIdx.x < dkv_groups) dkv_group<HD, KG>(g, smem_bwd, blockIdx.x);
+    else dq_group<HD>(g, smem_bwd, blockIdx.x - dkv_groups);
+}
+
+template <int HD, int KG>
+hipError_t launch_bwd(hipStream_t st, const AttnBwdArgs& b, const PackedShape& a) {
+    constexpr int LDS = std::max(DqCfg<HD>::LDS, DkvCfg<HD, KG>::LDS);
+    static LdsLimitOnce lim;
+    hipError_t e = lim.set(reinterpret_cast<const void*>(attn_packed_bwd_kernel<HD, KG>), LDS);
+    if (e != hipSuccess) return e;
+    const float scale = 1.0f / sqrtf((float)HD);
+    const BwdDev g{b.qkv, b.dO, b.lse, b.delta, b.dqkv, a.cu, a.n, a.T, a.Hq, a.Hkv, a.causal, scale, scale * LOG2E};
+    const long kv = (((long)a.T / (32 * KG) + a.n) * a.Hkv + 7) / 8 * 8;         // ids of either kind begin on the first XCD
+    const bool two = a.Hq / a.Hkv % 2 == 0;
+    const long q = ((long)a.T / (two ? 128 : 256) + a.n) * (two ? a.Hq / 2 : a.Hq);
+    attn_packed_bwd_kernel<HD, KG><<<dim3((unsigned)(kv + q)), BWD_WAVES * 64, LDS, st>>>(g, (int)kv);
+    return hipGetLastError();
+}
+
+template <int HD>
+hipError_t launch_hd(hipStream_t st, const AttnBwdArgs& b, const PackedShape& a) {
+    const char* e = getenv("PKG");
+    if (e && e[0] == '2') return launch_bwd<HD, 2>(st, b, a);
+    return launch_bwd<HD, 4>(st, b, a);
+}
+
+}  // namespace
+
+hipError_t spk_launch_attention_packed_bwd(hipStream_t st, const AttnBwdArgs& b, const PackedShape& a) {
+    switch (a.hd) {
+        case 64: return launch_hd<64>(st, b, a);
+        case 80: return launch_hd<80>(st, b, a);
+        case 128: return launch_hd<128>(st, b, a);
+        default: return hipErrorInvalidValue;
+    }
+}

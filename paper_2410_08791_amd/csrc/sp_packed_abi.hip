@@ -43,7 +43,7 @@ extern "C" int spk_batch_plan(void* stream, const int32_t* lens, const int32_t* 
 
 // Everything but the pointers; slots of 32 rows are the most that any form launches per head.
 static bool packed_ok(int n, int T, int Hq, int Hkv, int hd) {
-    return n >= 1 && n <= kPackedMaxSeqs && T >= 1 && T <= kMostPositions && Hkv >= 1 && Hq >= Hkv && Hq % Hkv == 0 && Hq <= 65535 &&
+    return n >= 1 && n <= kPackedMaxSeqs && T >= 1 && T <= kMostPositions && Hkv >= 1 && Hq >= Hkv && Hq % Hkv == 0 && Hq <= 16384 &&
            (hd == 64 || hd == 80 || hd == 128) && ((long)T / 32 + n) * Hq <= INT_MAX / 512;
 }
 
