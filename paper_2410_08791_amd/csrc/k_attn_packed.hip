@@ -20,6 +20,13 @@ typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ bf16x8_t lds_frag(const unsigned char* __restrict__ p) { return *reinterpret_cast<const bf16x8_t*>(p); }
 
+__device__ __forceinline__ f32x16_t zeros() {
+    f32x16_t z;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) z[e] = 0.f;
+    return z;
+}
+
 // Maximum of a value over the two half-waves.
 __device__ __forceinline__ float half_max(float v) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -84,10 +91,11 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void attn_packed_kernel
     // on top; rows of 192: two k-steps of four chunks are an offset.
     constexpr bool XOR = HD != 80;
     const int kp0 = l32 * C::ROWB + ((half ^ C::k_swz(l32)) << 4), kp1 = l32 * C::ROWB + (((2 | half) ^ C::k_swz(l32)) << 4);
-    auto k_at = [&](int base, int ks) { return XOR ? (base + kp0) ^ (ks << 5) : base + ((ks & 1) ? kp1 : kp0) + (ks >> 1) * 64; };
+    // Addresses are of the stage at `base`; what lies further on in it is a constant on top, which the read takes as its offset.
+    auto k_at = [&](int base, int ks) { return smem_packed + (XOR ? (base + kp0) ^ (ks << 5) : base + ((ks & 1) ? kp1 : kp0) + (ks >> 1) * 64); };
     const int rowv = half * 4 + ((lane & 15) >> 2);
     const int vp0 = rowv * C::ROWB + (C::v_swz(rowv) << 6) + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
-    auto v_at = [&](int base, int mt) { return XOR ? (base + vp0) ^ (mt << 6) : base + vp0 + mt * 64; };
+    auto v_at = [&](int base, int mt) { return smem_packed + (XOR ? (base + vp0) ^ (mt << 6) : base + vp0 + mt * 64); };
 
     const int q0 = pb.blk * QB, wq0 = q0 + wave * (MQ * 32), qi = wq0 + l32;
     bf16x8_t qf[MQ][C::NKS];
@@ -111,18 +119,16 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void attn_packed_kernel
     const int ntiles = ((causal ? min(len, q0 + QB) : len) + KB - 1) / KB;               // of the work-group
     const int mine = wq0 >= len ? 0 : ((causal ? min(len, wq0 + MQ * 32) : len) + KB - 1) / KB;   // of this wave
 
+    // Scores of a tile's first 32 keys, nothing beside them: all fragments are on their way before the first MFMA.
     auto scores = [&](int base, f32x16_t (&s)[MQ]) __attribute__((always_inline)) {
+        bf16x8_t kf[C::NKS];
 #pragma unroll
-        for (int ks = 0; ks < C::NKS; ++ks) {
-            const bf16x8_t kf = lds_frag(smem_packed + k_at(base, ks));
+        for (int ks = 0; ks < C::NKS; ++ks) kf[ks] = lds_frag(k_at(base, ks));
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int m = 0; m < MQ; ++m) {
-                if (ks == 0)
+        for (int ks = 0; ks < C::NKS; ++ks)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) s[m][e] = 0.f;
-                s[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[m][ks], s[m], 0, 0, 0);
-            }
-        }
+            for (int m = 0; m < MQ; ++m) s[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[m][ks], ks ? s[m] : zeros(), 0, 0, 0);
     };
     f32x16_t sa[MQ], sb[MQ];
     float alpha[MQ], mx[MQ];                 // mx: of the lane's 16 scores of the next step
@@ -165,14 +171,14 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void attn_packed_kernel
     // the maximum of the next.  The order is the source's: fragments are read PF ahead of the MFMA that takes them, and each
     // MFMA is followed by its share of the vector arithmetic (left to the compiler, every read was waited for at once; the
     // empty asm statements keep it from sinking the arithmetic to its use).
-    auto step = [&](f32x16_t (&s)[MQ], int base_v, f32x16_t (&s_next)[MQ], int base_k, bool next) __attribute__((always_inline)) {
-        constexpr int PF = 3, NK = C::NKS, NV = 2 * C::NMT;
+    auto step = [&](f32x16_t (&s)[MQ], f32x16_t (&s_next)[MQ], int base, int off_v, int off_k, bool next) __attribute__((always_inline)) {
+        constexpr int NK = C::NKS, NV = 2 * C::NMT, PF = NK < 5 ? NK : 5;
         u32x4_t p[MQ][2];
         bf16x8_t kf[NK], vf[NV];
         float m_scaled[MQ], sum[MQ];
-        auto kread = [&](int i) __attribute__((always_inline)) { kf[i] = lds_frag(smem_packed + k_at(base_k, i)); };
+        auto kread = [&](int i) __attribute__((always_inline)) { kf[i] = lds_frag(k_at(base, i) + off_k); };
         auto vread = [&](int i) __attribute__((always_inline)) {
-            const unsigned char* vp = smem_packed + v_at(base_v, i % C::NMT) + 16 * (i / C::NMT) * C::ROWB;
+            const unsigned char* vp = v_at(base, i % C::NMT) + off_v + 16 * (i / C::NMT) * C::ROWB;
             const s16x4_t lo = sp_tr_read((lds_s16x4_ptr)(vp));
             const s16x4_t hi = sp_tr_read((lds_s16x4_ptr)(vp + 8 * C::ROWB));
             vf[i] = __builtin_bit_cast(bf16x8_t, s16x8_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
@@ -184,8 +190,6 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void attn_packed_kernel
         for (int m = 0; m < MQ; ++m) {
             m_scaled[m] = m_run[m] * scale_log2e;
             sum[m] = 0.f;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s_next[m][e] = 0.f;
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -194,7 +198,7 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void attn_packed_kernel
             else if (next) kread(i + PF);
 #pragma unroll
             for (int m = 0; m < MQ; ++m)
-                if (next) s_next[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[m][i], s_next[m], 0, 0, 0);
+                if (next) s_next[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[m][i], i ? s_next[m] : zeros(), 0, 0, 0);
 #pragma unroll
             for (int m = 0; m < MQ; ++m)
 #pragma unroll
@@ -235,9 +239,9 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void attn_packed_kernel
     // two of four, 333 us for the 274 of 64/8 heads of 128 over 3333 + 130 + 1 + 1777 tokens.)
     auto body = [&](int cur, int key0, bool mask) __attribute__((always_inline)) {
         settle(sa, key0, mask);
-        step(sa, cur + C::TILE_BYTES, sb, cur + HALF, true);
+        step(sa, sb, cur, C::TILE_BYTES, HALF, true);
         settle(sb, key0 + 32, mask);
-        step(sb, cur + C::TILE_BYTES + HALF, sa, 0, false);
+        step(sb, sa, cur, C::TILE_BYTES + HALF, 0, false);
     };
     auto enter = [&](int kt) __attribute__((always_inline)) {
         // tile kt has landed, this wave's part by the wait, everybody's by the barrier; and everybody is done with tile kt - 1,

@@ -9,7 +9,6 @@
 // wave therefore reads its fragments a few MFMAs ahead, in an order that the source fixes, and works P beside the MFMAs
 // of dP, and dS beside those of dV (dk/dv) or of the next 32 keys' scores (dq).  One launch: a short batch has too few
 // blocks of either kind to fill the chip.
-#include <stdlib.h>
 #include "sp_attn.h"
 #include "sp_packed.h"
 
@@ -30,7 +29,8 @@ constexpr int step_of(int e, int n, int total) {
 }
 constexpr float LOG2E = 1.4426950408889634f;
 
-// Fragment addresses of a token tile (TokTile): the lane's part, the k-step or 32-row block on top.
+// Fragments of the token tiles (TokTile) of a stage: the lane's addresses in the stage's first tile, the k-step or 32-row
+// block on top; what lies further on in the stage is a constant, which the read takes as its offset.
 template <int HD>
 struct FragAt {
     typedef TokTile<HD> T;
@@ -41,13 +41,13 @@ struct FragAt {
         t0 = T::tr_pos(0, lane);
     }
     // rows of 128 and 256 bytes: an exclusive or; of 192: two k-steps of four chunks, or a block, are an offset
-    __device__ bf16x8_t row(const unsigned char* smem, int base, int ks) const {
-        return lds_b128(smem + (HD != 80 ? (base + r0) ^ (ks << 5) : base + ((ks & 1) ? r1 : r0) + (ks >> 1) * 64));
+    __device__ __forceinline__ bf16x8_t row(const unsigned char* smem, int base, int ks, int off) const {
+        return lds_b128(smem + (HD != 80 ? (base + r0) ^ (ks << 5) : base + ((ks & 1) ? r1 : r0) + (ks >> 1) * 64) + off);
     }
-    __device__ bf16x8_t tr(const unsigned char* smem, int base, int mt) const {
+    __device__ __forceinline__ bf16x8_t tr(const unsigned char* smem, int base, int mt, int off) const {
         const int a = HD != 80 ? (base + t0) ^ (mt << 6) : base + t0 + mt * 64;
-        const s16x4_t lo = sp_tr_read((lds_s16x4_ptr)(smem + a));
-        const s16x4_t hi = sp_tr_read((lds_s16x4_ptr)(smem + (a ^ 32) + 8 * T::ROWB));
+        const s16x4_t lo = sp_tr_read((lds_s16x4_ptr)(smem + a + off));
+        const s16x4_t hi = sp_tr_read((lds_s16x4_ptr)(smem + (a ^ 32) + off + 8 * T::ROWB));
         return __builtin_bit_cast(bf16x8_t, s16x8_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
     }
 };
@@ -81,10 +81,12 @@ struct TileLoad {
     }
 };
 
+constexpr int STAGES = 3;                     // tiles under way: the one that is worked, two that are loading
+// A wave's loads but the last IN_FLIGHT have landed; behind the barrier every wave's have.
+template <int IN_FLIGHT>
 __device__ __forceinline__ void landed() {
-    // this wave's loads and LDS accesses; behind the barrier every wave's
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(sp_waitcnt(0, 0));
+    __builtin_amdgcn_s_waitcnt(sp_waitcnt(IN_FLIGHT, 15));
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
@@ -111,7 +113,7 @@ __device__ __forceinline__ int near_heads(int i, int heads) { return heads & 7 ?
 template <int HD>
 struct DqCfg {
     typedef TokTile<HD> T;
-    static constexpr int STAGE = 2 * T::BYTES, LDS = 2 * STAGE;      // {K, V} of 64 keys
+    static constexpr int STAGE = 2 * T::BYTES, LDS = STAGES * STAGE;      // {K, V} of 64 keys
 };
 
 template <int HD>
@@ -138,11 +140,10 @@ __device__ __forceinline__ void dq_group(const BwdDev& g, unsigned char* smem, i
     TileLoad<HD, KEYS> tl;
     tl.init(wave, lane);
     auto issue = [&](int t) __attribute__((always_inline)) {
-        unsigned char* st = smem + (t & 1) * C::STAGE;
+        unsigned char* st = smem + t % STAGES * C::STAGE;
         tl.issue(st, wave, kbase + (size_t)t * KEYS * ld, ld, len - t * KEYS);
         tl.issue(st + T::BYTES, wave, vbase + (size_t)t * KEYS * ld, ld, len - t * KEYS);
     };
-    issue(0);
     bf16x8_t qf[NK], dof[NK];
     {
         const bf16_t* qp = g.qkv + (tok0 + qr) * ld + h * HD + half * 8;
@@ -154,6 +155,8 @@ __device__ __forceinline__ void dq_group(const BwdDev& g, unsigned char* smem, i
         }
     }
     const float lse_q = g.lse[row0 + qr] * LOG2E, delta_q = g.delta[row0 + qr];
+    issue(0);
+    if (ntiles > 1) issue(1);
     FragAt<HD> at;
     at.init(lane);
     f32x16_t acc[T::NMT];
@@ -166,16 +169,15 @@ __device__ __forceinline__ void dq_group(const BwdDev& g, unsigned char* smem, i
         for (int e = 0; e < 16; ++e) s[e] = (e >> 2) * 8 + (e & 3) <= last ? s[e] : -INFINITY;
     };
     // 32 keys: dP beside P (which takes the place of the scores), from the V rows at base_v
-    auto probs = [&](f32x16_t& s, f32x16_t& dp, int base_v) __attribute__((always_inline)) {
+    auto probs = [&](f32x16_t& s, f32x16_t& dp, int base, int off) __attribute__((always_inline)) {
         bf16x8_t vf[NK];
 #pragma unroll
-        for (int i = 0; i < PF; ++i) vf[i] = at.row(smem, base_v, i);
-        dp = zeros();
+        for (int i = 0; i < PF; ++i) vf[i] = at.row(smem, base, i, off);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < NK; ++i) {
-            if (i + PF < NK) vf[i + PF] = at.row(smem, base_v, i + PF);
-            dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i], dof[i], dp, 0, 0, 0);
+            if (i + PF < NK) vf[i + PF] = at.row(smem, base, i + PF, off);
+            dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i], dof[i], i ? dp : zeros(), 0, 0, 0);
 #pragma unroll
             for (int e = 16 * i / NK; e < 16 * (i + 1) / NK; ++e) {
                 float p = __builtin_amdgcn_exp2f(fmaf(s[e], g.scale_log2e, -lse_q));
@@ -186,19 +188,18 @@ __device__ __forceinline__ void dq_group(const BwdDev& g, unsigned char* smem, i
         }
     };
     // dS of 32 keys (P in s) beside the next scores, if any, from the K rows at base_k
-    auto grads = [&](const f32x16_t& s, const f32x16_t& dp, u32x4_t (&ds)[2], f32x16_t& s_next, int base_k, bool next) __attribute__((always_inline)) {
+    auto grads = [&](const f32x16_t& s, const f32x16_t& dp, u32x4_t (&ds)[2], f32x16_t& s_next, int base, int off, bool next) __attribute__((always_inline)) {
         bf16x8_t kf[NK];
         if (next) {
 #pragma unroll
-            for (int i = 0; i < PF; ++i) kf[i] = at.row(smem, base_k, i);
-            s_next = zeros();
+            for (int i = 0; i < PF; ++i) kf[i] = at.row(smem, base, i, off);
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < NK; ++i) {
             if (next) {
-                if (i + PF < NK) kf[i + PF] = at.row(smem, base_k, i + PF);
-                s_next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[i], s_next, 0, 0, 0);
+                if (i + PF < NK) kf[i + PF] = at.row(smem, base, i + PF, off);
+                s_next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[i], i ? s_next : zeros(), 0, 0, 0);
             }
 #pragma unroll
             for (int e = 8 * i / NK; e < 8 * (i + 1) / NK; ++e) {
@@ -209,9 +210,9 @@ __device__ __forceinline__ void dq_group(const BwdDev& g, unsigned char* smem, i
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    auto output = [&](const u32x4_t (&ds)[2], int base) __attribute__((always_inline)) {
+    auto output = [&](const u32x4_t (&ds)[2], int base, int off) __attribute__((always_inline)) {
         bf16x8_t tf[NV];
-        auto read = [&](int i) __attribute__((always_inline)) { tf[i] = at.tr(smem, base + 16 * (i / T::NMT) * T::ROWB, i % T::NMT); };
+        auto read = [&](int i) __attribute__((always_inline)) { tf[i] = at.tr(smem, base, i % T::NMT, off + 16 * (i / T::NMT) * T::ROWB); };
 #pragma unroll
         for (int i = 0; i < PF; ++i) read(i);
         __builtin_amdgcn_sched_barrier(0);
@@ -224,36 +225,32 @@ __device__ __forceinline__ void dq_group(const BwdDev& g, unsigned char* smem, i
     };
     auto tile = [&](int t, bool mask) __attribute__((always_inline)) {
         constexpr int HALF = 32 * T::ROWB;
-        const int k = (t & 1) * C::STAGE, v = k + T::BYTES;
+        const int st = t % STAGES * C::STAGE;
         f32x16_t sa, sb, dp;
         u32x4_t ds[2];
         {
             bf16x8_t kf[NK];
 #pragma unroll
-            for (int i = 0; i < PF; ++i) kf[i] = at.row(smem, k, i);
-            sa = zeros();
+            for (int i = 0; i < NK; ++i) kf[i] = at.row(smem, st, i, 0);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < NK; ++i) {
-                if (i + PF < NK) kf[i + PF] = at.row(smem, k, i + PF);
-                sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[i], sa, 0, 0, 0);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            for (int i = 0; i < NK; ++i) sa = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[i], i ? sa : zeros(), 0, 0, 0);
         }
         if (mask) mask_scores(sa, t * KEYS);
-        probs(sa, dp, v);
-        grads(sa, dp, ds, sb, k + HALF, true);
-        output(ds, k);
+        probs(sa, dp, st, T::BYTES);
+        grads(sa, dp, ds, sb, st, HALF, true);
+        output(ds, st, 0);
         if (mask) mask_scores(sb, t * KEYS + 32);
-        probs(sb, dp, v + HALF);
-        grads(sb, dp, ds, sa, 0, false);
-        output(ds, k + HALF);
+        probs(sb, dp, st, T::BYTES + HALF);
+        grads(sb, dp, ds, sa, st, 0, false);
+        output(ds, st, HALF);
     };
     // one barrier per tile for every wave; the diagonal and a ragged end lie in a wave's last tile
     int t = 0;
     auto enter = [&]() __attribute__((always_inline)) {
-        landed();
-        if (t + 1 < ntiles) issue(t + 1);
+        if (t + 1 < ntiles) landed<2 * TileLoad<HD, KEYS>::NI>();
+        else landed<0>();
+        if (t + 2 < ntiles) issue(t + 2);
     };
     enter();
     if (mine > 0) {
@@ -292,8 +289,9 @@ struct DkvCfg {
     static constexpr bool K_IN_LDS = HD == 128;       // K fragments would not fit beside the accumulators
     static constexpr int TILE = ROWS * T::ROWB, STAGE = 2 * TILE;
     static constexpr int KBYTES = K_IN_LDS ? KEYS * T::ROWB : 0;
-    static constexpr int LDS = 2 * STAGE + KBYTES + 2 * 2 * ROWS * 4;
+    static constexpr int LDS = STAGES * STAGE + KBYTES + STAGES * 2 * ROWS * 4;
     static_assert((SUBS - 1) * KG * T::NMT * 16 * 256 <= 2 * STAGE, "the parts' sums fit the stages");
+    static_assert(ROWS == 64, "a row value per lane");
     static_assert(LDS <= 160 * 1024, "fits the LDS");
 };
 
@@ -315,41 +313,36 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
     const size_t tok0 = pb.row0;
     const bf16_t* kbase = g.qkv + tok0 * ld + (size_t)(Hq + kvh) * HD;
     const bf16_t* vbase = kbase + (size_t)Hkv * HD;
-    unsigned char* sKeys = smem + 2 * C::STAGE;
-    float* rowvals = reinterpret_cast<float*>(smem + 2 * C::STAGE + C::KBYTES);       // [stage][lse | delta][ROWS]
+    unsigned char* sKeys = smem + STAGES * C::STAGE;
+    float* rowvals = reinterpret_cast<float*>(smem + STAGES * C::STAGE + C::KBYTES);       // [stage][lse | delta][ROWS]
 
     // the tiles in walking order: (query head of the group, ROWS queries)
     const int q_begin = g.causal ? k0 / C::ROWS * C::ROWS : 0;
     const int per_head = (len - q_begin + C::ROWS - 1) / C::ROWS, n_tiles = grp * per_head;
     TileLoad<HD, C::ROWS> tl;
     tl.init(wave, lane);
-    float r_lse = 0.f, r_delta = 0.f;
     int f_head = 0, f_q = q_begin;                    // of the tile fetched next
-    auto fetch = [&](int tile) __attribute__((always_inline)) {
+    auto fetch = [&](int stage) __attribute__((always_inline)) {
         const int h = kvh * grp + f_head;
-        unsigned char* st = smem + (tile & 1) * C::STAGE;
+        unsigned char* st = smem + stage * C::STAGE;
         tl.issue(st, wave, g.qkv + (tok0 + f_q) * ld + (size_t)h * HD, ld, len - f_q);
         tl.issue(st + C::TILE, wave, g.dO + (tok0 + f_q) * ld_do + (size_t)h * HD, ld_do, len - f_q);
-        if (threadIdx.x < C::ROWS) {
-            const size_t row = (size_t)h * g.T + tok0 + min(f_q + (int)threadIdx.x, len - 1);
-            r_lse = g.lse[row] * LOG2E;
-            r_delta = g.delta[row];
+        // wave 0 the rows' log-sum-exps, wave 1 their deltas
+#if defined(__HIP_DEVICE_COMPILE__)
+        if (wave < 2) {
+            const float* src = (wave ? g.delta : g.lse) + (size_t)h * g.T + tok0 + f_q;
+            const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(src), 0, min(len - f_q, C::ROWS) * 4, 0x00020000);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void_ptr)(rowvals + (stage * 2 + wave) * C::ROWS), 4, lane * 4, 0, 0, 0);
         }
+#endif
         f_q += C::ROWS;
         if (f_q >= len) { f_q = q_begin; ++f_head; }
-    };
-    auto put_rowvals = [&](int tile) __attribute__((always_inline)) {
-        if (threadIdx.x < C::ROWS) {
-            rowvals[(tile & 1) * 2 * C::ROWS + threadIdx.x] = r_lse;
-            rowvals[(tile & 1) * 2 * C::ROWS + C::ROWS + threadIdx.x] = r_delta;
-        }
     };
     if (C::K_IN_LDS) {
         TileLoad<HD, C::KEYS> kl;
         kl.init(wave, lane);
         kl.issue(sKeys, wave, kbase + (size_t)k0 * ld, ld, len - k0);
     }
-    fetch(0);
     bf16x8_t kf_reg[C::K_IN_LDS ? 1 : NK], vf[NK];
     {
         const size_t kr = min(kj, len - 1);
@@ -365,22 +358,26 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
 #pragma unroll
     for (int t = 0; t < T::NMT; ++t) { dk[t] = zeros(); dv[t] = zeros(); }
 
-    put_rowvals(0);
-    landed();
+    fetch(0);
+    if (n_tiles > 1) fetch(1);
     int qs = q_begin + sub * 32;                      // this wave's first query of the tile
-    for (int tile = 0; tile < n_tiles; ++tile) {
-        const bool more = tile + 1 < n_tiles;
-        if (more) fetch(tile + 1);
-        const int q_at = (tile & 1) * C::STAGE + sub * 32 * T::ROWB, do_at = q_at + C::TILE;
-        const float* lrow = rowvals + (tile & 1) * 2 * C::ROWS + sub * 32 + half * 4;
+    constexpr int NL = 2 * TileLoad<HD, C::ROWS>::NI; // a wave's loads of a tile, without the row values
+    for (int tile = 0, stage = 0; tile < n_tiles; ++tile) {
+        // the tile is there; everybody is done with the one before it, whose stage the tile after next takes
+        if (tile + 1 == n_tiles) landed<0>();
+        else if (wave < 2) landed<NL + 1>();
+        else landed<NL>();
+        if (tile + 2 < n_tiles) fetch(stage ? stage - 1 : STAGES - 1);
+        const int q_at = stage * C::STAGE + sub * 32 * T::ROWB;
+        const float* lrow = rowvals + stage * 2 * C::ROWS + sub * 32 + half * 4;
         // wave-uniform skips: every query of the part precedes this wave's keys, none exists, no key exists
         if (!(qs >= len || wk0 >= len || (g.causal && qs + 31 < wk0))) {
-            f32x16_t s = zeros(), dp;
+            f32x16_t s, dp;
             {
                 bf16x8_t qf[NK], kf[NK];
                 auto read = [&](int i) __attribute__((always_inline)) {
-                    qf[i] = at.row(smem, q_at, i);
-                    if (C::K_IN_LDS) kf[i] = at.row(sKeys, kg * 32 * T::ROWB, i);
+                    qf[i] = at.row(smem, q_at, i, 0);
+                    if (C::K_IN_LDS) kf[i] = at.row(sKeys, kg * 32 * T::ROWB, i, 0);
                 };
 #pragma unroll
                 for (int i = 0; i < PF; ++i) read(i);
@@ -388,7 +385,7 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
 #pragma unroll
                 for (int i = 0; i < NK; ++i) {
                     if (i + PF < NK) read(i + PF);
-                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[i], C::K_IN_LDS ? kf[i] : kf_reg[C::K_IN_LDS ? 0 : i], s, 0, 0, 0);
+                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[i], C::K_IN_LDS ? kf[i] : kf_reg[C::K_IN_LDS ? 0 : i], i ? s : zeros(), 0, 0, 0);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -406,23 +403,22 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
             {
                 bf16x8_t df[NK];
                 float4 l4[4];
-                dp = zeros();
                 l4[0] = lds_f4(lrow);                    // the others a step ahead of their use: registers are short here
 #pragma unroll
-                for (int i = 0; i < PF; ++i) df[i] = at.row(smem, do_at, i);
+                for (int i = 0; i < PF; ++i) df[i] = at.row(smem, q_at, i, C::TILE);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int i = 0; i < NK; ++i) {
-                    if (i + PF < NK) df[i + PF] = at.row(smem, do_at, i + PF);
+                    if (i + PF < NK) df[i + PF] = at.row(smem, q_at, i + PF, C::TILE);
 #pragma unroll
                     for (int k = 1; k < 4; ++k)
                         if (step_of(2 * k, NK, 8) == i + 1) l4[k] = lds_f4(lrow + k * 8);
-                    dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(df[i], vf[i], dp, 0, 0, 0);
+                    dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(df[i], vf[i], i ? dp : zeros(), 0, 0, 0);
 #pragma unroll
                     for (int e = 8 * i / NK; e < 8 * (i + 1) / NK; ++e) {
                         const float4 l = l4[e >> 1];
-                        const float a = __builtin_amdgcn_exp2f(fmaf(s[2 * e], g.scale_log2e, -((e & 1) ? l.z : l.x)));
-                        const float b = __builtin_amdgcn_exp2f(fmaf(s[2 * e + 1], g.scale_log2e, -((e & 1) ? l.w : l.y)));
+                        const float a = __builtin_amdgcn_exp2f(fmaf(s[2 * e], g.scale_log2e, -LOG2E * ((e & 1) ? l.z : l.x)));
+                        const float b = __builtin_amdgcn_exp2f(fmaf(s[2 * e + 1], g.scale_log2e, -LOG2E * ((e & 1) ? l.w : l.y)));
                         uint32_t w = pack2(a, b);
                         asm volatile("" : "+v"(w));
                         pw[e >> 2][e & 3] = w;
@@ -435,7 +431,7 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
             {
                 bf16x8_t tf[NV];
                 float4 d4[4];
-                auto read = [&](int i) __attribute__((always_inline)) { tf[i] = at.tr(smem, do_at + 16 * (i / T::NMT) * T::ROWB, i % T::NMT); };
+                auto read = [&](int i) __attribute__((always_inline)) { tf[i] = at.tr(smem, q_at, i % T::NMT, C::TILE + 16 * (i / T::NMT) * T::ROWB); };
                 d4[0] = lds_f4(lrow + C::ROWS);
 #pragma unroll
                 for (int i = 0; i < PF; ++i) read(i);
@@ -459,7 +455,7 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
             }
             {
                 bf16x8_t tf[NV];
-                auto read = [&](int i) __attribute__((always_inline)) { tf[i] = at.tr(smem, q_at + 16 * (i / T::NMT) * T::ROWB, i % T::NMT); };
+                auto read = [&](int i) __attribute__((always_inline)) { tf[i] = at.tr(smem, q_at, i % T::NMT, 16 * (i / T::NMT) * T::ROWB); };
 #pragma unroll
                 for (int i = 0; i < PF; ++i) read(i);
                 __builtin_amdgcn_sched_barrier(0);
@@ -473,9 +469,9 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
         }
         qs += C::ROWS;
         if (qs - sub * 32 >= len) qs = q_begin + sub * 32;
-        if (more) put_rowvals(tile + 1);
-        landed();
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
     }
+    landed<0>();
     // The parts' sums meet in the stages: dK in part 0, dV in part 1, added in the order of the parts.
     float4* x = reinterpret_cast<float4*>(smem) + lane;
     auto place = [&](int s, int owner) { return ((s < owner ? s : s - 1) * KG + kg) * (T::NMT * 4 * 64); };
@@ -538,8 +534,6 @@ hipError_t launch_bwd(hipStream_t st, const AttnBwdArgs& b, const PackedShape& a
 
 template <int HD>
 hipError_t launch_hd(hipStream_t st, const AttnBwdArgs& b, const PackedShape& a) {
-    const char* e = getenv("PKG");
-    if (e && e[0] == '2') return launch_bwd<HD, 2>(st, b, a);
     return launch_bwd<HD, 4>(st, b, a);
 }
 
