@@ -1,14 +1,15 @@
 // Backward of the attention over packed prompts: dq, dk, dv from q, k, v, dO, the forward's log-sum-exp and
 // delta = rowsum(dO * O), without atomics, in one launch of two kinds of work-groups that do not depend on one another:
-//   dk/dv -- a work-group owns 32 KG keys of one key/value head and walks the queries of every query head that shares it;
-//   dq    -- a work-group owns 256 queries of one head, or 128 of two heads that share keys and values, and walks the keys.
+//   dk/dv -- a work-group owns 128 keys of one key/value head and walks the queries of every query head that shares it;
+//   dq    -- a work-group owns 128 queries of one head and walks the keys.
 // P = exp(s - lse), dS = P (dP - delta), dP = dO V^T; layouts and tiles are those of k_attn_bwd.hip.
 //
 // What bounds it: 7 products of 2 hd flops per pair of a query and a key on the matrix pipe, 1 KB of LDS per MFMA of 32
 // cycles (which four SIMDs drawing at once would all but use up), and the arithmetic of P and dS on the vector pipe.  Every
 // wave therefore reads its fragments a few MFMAs ahead, in an order that the source fixes, and works P beside the MFMAs
 // of dP, and dS beside those of dV (dk/dv) or of the next 32 keys' scores (dq).  One launch: a short batch has too few
-// blocks of either kind to fill the chip.
+// blocks of either kind to fill the chip.  Four waves each, two work-groups per CU: with one of eight, nothing covered
+// the other's first loads and last stores.
 #include "sp_attn.h"
 #include "sp_packed.h"
 
@@ -20,7 +21,7 @@ __device__ __forceinline__ bf16x8_t lds_b128(const unsigned char* __restrict__ p
 __device__ __forceinline__ float4 lds_f4(const float* __restrict__ p) { return *reinterpret_cast<const float4*>(p); }
 __device__ __forceinline__ uint32_t pack2(float a, float b) { return __builtin_bit_cast(uint32_t, bf16x2_t{(__bf16)a, (__bf16)b}); }
 
-constexpr int BWD_WAVES = 8;
+constexpr int BWD_WAVES = 4;
 // The one of n steps that share out `total` items evenly which takes item e.
 constexpr int step_of(int e, int n, int total) {
     int i = 0;
@@ -52,7 +53,7 @@ struct FragAt {
     }
 };
 
-// Loads of a tile of ROWS token rows by eight waves, straight into LDS.  Rows past those that exist and the padding of
+// Loads of a tile of ROWS token rows by a work-group, straight into LDS.  Rows past those that exist and the padding of
 // 192-byte rows lie outside the buffer that the load is given and land as zeros.
 template <int HD, int ROWS>
 struct TileLoad {
@@ -81,7 +82,8 @@ struct TileLoad {
     }
 };
 
-constexpr int STAGES = 3;                     // tiles under way: the one that is worked, two that are loading
+template <int HD>
+constexpr int STAGES = HD == 128 ? 2 : 3;     // tiles under way: the one that is worked, and those that are loading
 // A wave's loads but the last IN_FLIGHT have landed; behind the barrier every wave's have.
 template <int IN_FLIGHT>
 __device__ __forceinline__ void landed() {
@@ -113,7 +115,7 @@ __device__ __forceinline__ int near_heads(int i, int heads) { return heads & 7 ?
 template <int HD>
 struct DqCfg {
     typedef TokTile<HD> T;
-    static constexpr int STAGE = 2 * T::BYTES, LDS = STAGES * STAGE;      // {K, V} of 64 keys
+    static constexpr int STAGE = 2 * T::BYTES, LDS = STAGES<HD> * STAGE;      // {K, V} of 64 keys
 };
 
 template <int HD>
@@ -124,23 +126,21 @@ __device__ __forceinline__ void dq_group(const BwdDev& g, unsigned char* smem, i
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, half = lane >> 5;
     const int Hq = g.Hq, Hkv = g.Hkv, grp = Hq / Hkv, ld = (Hq + 2 * Hkv) * HD;
-    const bool two = grp % 2 == 0;                    // two heads of 128 queries
-    const int units = two ? Hq / 2 : Hq, slot = id / units, unit = near_heads(id - slot * units, units);
-    const int h = two ? unit * 2 + (wave >> 2) : unit;
-    const PackedBlock pb = two ? packed_block<128>(g.cu, g.n, g.T, slot) : packed_block<256>(g.cu, g.n, g.T, slot);
-    const int rows = two ? 128 : 256, q0 = pb.blk * rows, len = pb.len;
+    const int slot = id / Hq, h = near_heads(id - slot * Hq, Hq);
+    const PackedBlock pb = packed_block<128>(g.cu, g.n, g.T, slot);
+    const int q0 = pb.blk * 128, len = pb.len;
     if (q0 >= len) return;
-    const int wq0 = q0 + (two ? wave & 3 : wave) * 32, qi = wq0 + l32;
+    const int wq0 = q0 + wave * 32, qi = wq0 + l32;
     const size_t tok0 = pb.row0, row0 = (size_t)h * g.T + tok0;
     const int qr = min(qi, len - 1);
     const bf16_t* kbase = g.qkv + tok0 * ld + (size_t)(Hq + h / grp) * HD;
     const bf16_t* vbase = kbase + (size_t)Hkv * HD;
-    const int ntiles = ((g.causal ? min(len, q0 + rows) : len) + KEYS - 1) / KEYS;
+    const int ntiles = ((g.causal ? min(len, q0 + 128) : len) + KEYS - 1) / KEYS;
     const int mine = wq0 >= len ? 0 : ((g.causal ? min(len, wq0 + 32) : len) + KEYS - 1) / KEYS;
     TileLoad<HD, KEYS> tl;
     tl.init(wave, lane);
     auto issue = [&](int t) __attribute__((always_inline)) {
-        unsigned char* st = smem + t % STAGES * C::STAGE;
+        unsigned char* st = smem + t % STAGES<HD> * C::STAGE;
         tl.issue(st, wave, kbase + (size_t)t * KEYS * ld, ld, len - t * KEYS);
         tl.issue(st + T::BYTES, wave, vbase + (size_t)t * KEYS * ld, ld, len - t * KEYS);
     };
@@ -156,7 +156,7 @@ __device__ __forceinline__ void dq_group(const BwdDev& g, unsigned char* smem, i
     }
     const float lse_q = g.lse[row0 + qr] * LOG2E, delta_q = g.delta[row0 + qr];
     issue(0);
-    if (ntiles > 1) issue(1);
+    if (STAGES<HD> > 2 && ntiles > 1) issue(1);
     FragAt<HD> at;
     at.init(lane);
     f32x16_t acc[T::NMT];
@@ -225,7 +225,7 @@ __device__ __forceinline__ void dq_group(const BwdDev& g, unsigned char* smem, i
     };
     auto tile = [&](int t, bool mask) __attribute__((always_inline)) {
         constexpr int HALF = 32 * T::ROWB;
-        const int st = t % STAGES * C::STAGE;
+        const int st = t % STAGES<HD> * C::STAGE;
         f32x16_t sa, sb, dp;
         u32x4_t ds[2];
         {
@@ -248,9 +248,9 @@ __device__ __forceinline__ void dq_group(const BwdDev& g, unsigned char* smem, i
     // one barrier per tile for every wave; the diagonal and a ragged end lie in a wave's last tile
     int t = 0;
     auto enter = [&]() __attribute__((always_inline)) {
-        if (t + 1 < ntiles) landed<2 * TileLoad<HD, KEYS>::NI>();
+        if (STAGES<HD> > 2 && t + 1 < ntiles) landed<2 * TileLoad<HD, KEYS>::NI>();
         else landed<0>();
-        if (t + 2 < ntiles) issue(t + 2);
+        if (t + STAGES<HD> - 1 < ntiles) issue(t + STAGES<HD> - 1);
     };
     enter();
     if (mine > 0) {
@@ -280,28 +280,26 @@ __device__ __forceinline__ void dq_group(const BwdDev& g, unsigned char* smem, i
 }
 
 // ---------------------------------------------------------------------------------------------- dk, dv
-// Wave w takes the 32 keys of group w % KG (one key per lane as the B operand of S = Q K^T and dP = dO V^T) against the 32
-// queries of part w / KG of each tile; the parts' sums are added through LDS at the end.
-template <int HD, int KG>
+// Wave w takes the 32 keys of group w (one key per lane as the B operand of S = Q K^T and dP = dO V^T) against each tile of 32
+// queries.
+template <int HD>
 struct DkvCfg {
     typedef TokTile<HD> T;
-    static constexpr int SUBS = BWD_WAVES / KG, ROWS = 32 * SUBS, KEYS = 32 * KG;
+    static constexpr int ROWS = 32, KEYS = 128;
     static constexpr bool K_IN_LDS = HD == 128;       // K fragments would not fit beside the accumulators
     static constexpr int TILE = ROWS * T::ROWB, STAGE = 2 * TILE;
     static constexpr int KBYTES = K_IN_LDS ? KEYS * T::ROWB : 0;
-    static constexpr int LDS = STAGES * STAGE + KBYTES + STAGES * 2 * ROWS * 4;
-    static_assert((SUBS - 1) * KG * T::NMT * 16 * 256 <= 2 * STAGE, "the parts' sums fit the stages");
-    static_assert(ROWS == 64, "a row value per lane");
-    static_assert(LDS <= 160 * 1024, "fits the LDS");
+    static constexpr int LDS = STAGES<HD> * STAGE + KBYTES + STAGES<HD> * 2 * ROWS * 4;
+    static_assert(LDS <= 80 * 1024 && DqCfg<HD>::LDS <= 80 * 1024, "two work-groups fit a CU");
 };
 
-template <int HD, int KG>
+template <int HD>
 __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, int id) {
     typedef TokTile<HD> T;
-    typedef DkvCfg<HD, KG> C;
+    typedef DkvCfg<HD> C;
     constexpr int NK = T::NKS, NV = 2 * T::NMT, PF = 2;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int l32 = lane & 31, half = lane >> 5, kg = wave % KG, sub = wave / KG;
+    const int l32 = lane & 31, half = lane >> 5;
     const int Hq = g.Hq, Hkv = g.Hkv, grp = Hq / Hkv, ld = (Hq + 2 * Hkv) * HD, ld_do = Hq * HD;
     const int slot = id / Hkv, kvh = near_heads(id - slot * Hkv, Hkv);
     const PackedBlock pb = packed_block<C::KEYS>(g.cu, g.n, g.T, slot);
@@ -309,15 +307,15 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
     if (pb.blk * C::KEYS >= len) return;
     // under a causal mask the first block has the most queries
     const int blk = g.causal ? (len - 1) / C::KEYS - pb.blk : pb.blk;
-    const int k0 = blk * C::KEYS, wk0 = k0 + kg * 32, kj = wk0 + l32;
+    const int k0 = blk * C::KEYS, wk0 = k0 + wave * 32, kj = wk0 + l32;
     const size_t tok0 = pb.row0;
     const bf16_t* kbase = g.qkv + tok0 * ld + (size_t)(Hq + kvh) * HD;
     const bf16_t* vbase = kbase + (size_t)Hkv * HD;
-    unsigned char* sKeys = smem + STAGES * C::STAGE;
-    float* rowvals = reinterpret_cast<float*>(smem + STAGES * C::STAGE + C::KBYTES);       // [stage][lse | delta][ROWS]
+    unsigned char* sKeys = smem + STAGES<HD> * C::STAGE;
+    float* rowvals = reinterpret_cast<float*>(smem + STAGES<HD> * C::STAGE + C::KBYTES);       // [stage][lse | delta][ROWS]
 
     // the tiles in walking order: (query head of the group, ROWS queries)
-    const int q_begin = g.causal ? k0 / C::ROWS * C::ROWS : 0;
+    const int q_begin = g.causal ? k0 : 0;
     const int per_head = (len - q_begin + C::ROWS - 1) / C::ROWS, n_tiles = grp * per_head;
     TileLoad<HD, C::ROWS> tl;
     tl.init(wave, lane);
@@ -329,7 +327,7 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
         tl.issue(st + C::TILE, wave, g.dO + (tok0 + f_q) * ld_do + (size_t)h * HD, ld_do, len - f_q);
         // wave 0 the rows' log-sum-exps, wave 1 their deltas
 #if defined(__HIP_DEVICE_COMPILE__)
-        if (wave < 2) {
+        if (wave < 2 && lane < C::ROWS) {
             const float* src = (wave ? g.delta : g.lse) + (size_t)h * g.T + tok0 + f_q;
             const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(src), 0, min(len - f_q, C::ROWS) * 4, 0x00020000);
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void_ptr)(rowvals + (stage * 2 + wave) * C::ROWS), 4, lane * 4, 0, 0, 0);
@@ -359,25 +357,25 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
     for (int t = 0; t < T::NMT; ++t) { dk[t] = zeros(); dv[t] = zeros(); }
 
     fetch(0);
-    if (n_tiles > 1) fetch(1);
-    int qs = q_begin + sub * 32;                      // this wave's first query of the tile
+    if (STAGES<HD> > 2 && n_tiles > 1) fetch(1);
+    int qs = q_begin;                                 // first query of the tile
     constexpr int NL = 2 * TileLoad<HD, C::ROWS>::NI; // a wave's loads of a tile, without the row values
     for (int tile = 0, stage = 0; tile < n_tiles; ++tile) {
-        // the tile is there; everybody is done with the one before it, whose stage the tile after next takes
-        if (tile + 1 == n_tiles) landed<0>();
+        // the tile is there; everybody is done with the one before it, whose stage the next fetch takes
+        if (STAGES<HD> == 2 || tile + 1 == n_tiles) landed<0>();
         else if (wave < 2) landed<NL + 1>();
         else landed<NL>();
-        if (tile + 2 < n_tiles) fetch(stage ? stage - 1 : STAGES - 1);
-        const int q_at = stage * C::STAGE + sub * 32 * T::ROWB;
-        const float* lrow = rowvals + stage * 2 * C::ROWS + sub * 32 + half * 4;
-        // wave-uniform skips: every query of the part precedes this wave's keys, none exists, no key exists
+        if (tile + STAGES<HD> - 1 < n_tiles) fetch(stage ? stage - 1 : STAGES<HD> - 1);
+        const int q_at = stage * C::STAGE;
+        const float* lrow = rowvals + stage * 2 * C::ROWS + half * 4;
+        // wave-uniform skips: every query of the tile precedes this wave's keys, no key exists
         if (!(qs >= len || wk0 >= len || (g.causal && qs + 31 < wk0))) {
             f32x16_t s, dp;
             {
                 bf16x8_t qf[NK], kf[NK];
                 auto read = [&](int i) __attribute__((always_inline)) {
                     qf[i] = at.row(smem, q_at, i, 0);
-                    if (C::K_IN_LDS) kf[i] = at.row(sKeys, kg * 32 * T::ROWB, i, 0);
+                    if (C::K_IN_LDS) kf[i] = at.row(sKeys, wave * 32 * T::ROWB, i, 0);
                 };
 #pragma unroll
                 for (int i = 0; i < PF; ++i) read(i);
@@ -468,82 +466,54 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
             }
         }
         qs += C::ROWS;
-        if (qs - sub * 32 >= len) qs = q_begin + sub * 32;
-        stage = stage + 1 == STAGES ? 0 : stage + 1;
+        if (qs >= len) qs = q_begin;
+        stage = stage + 1 == STAGES<HD> ? 0 : stage + 1;
     }
-    landed<0>();
-    // The parts' sums meet in the stages: dK in part 0, dV in part 1, added in the order of the parts.
-    float4* x = reinterpret_cast<float4*>(smem) + lane;
-    auto place = [&](int s, int owner) { return ((s < owner ? s : s - 1) * KG + kg) * (T::NMT * 4 * 64); };
-    auto give = [&](const f32x16_t* a, int owner) {
-        if (sub == owner) return;
-#pragma unroll
-        for (int t = 0; t < T::NMT; ++t)
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                x[place(sub, owner) + (t * 4 + k) * 64] = make_float4(a[t][k * 4], a[t][k * 4 + 1], a[t][k * 4 + 2], a[t][k * 4 + 3]);
-    };
-    auto take = [&](const f32x16_t* a, int owner, int col, float f) {
-        if (sub != owner || kj >= len) return;
-        bf16_t* out = g.dqkv + (tok0 + kj) * ld + (size_t)(Hq + col + kvh) * HD;
+    if (kj >= len) return;
+    bf16_t* out = g.dqkv + (tok0 + kj) * ld + (size_t)(Hq + kvh) * HD;
+    auto store = [&](const f32x16_t* a, bf16_t* to, float f) {
 #pragma unroll
         for (int t = 0; t < T::NMT; ++t)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                float v[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int s = 0; s < C::SUBS; ++s) {
-                    const float4 o = s == owner ? make_float4(a[t][k * 4], a[t][k * 4 + 1], a[t][k * 4 + 2], a[t][k * 4 + 3])
-                                                : x[place(s, owner) + (t * 4 + k) * 64];
-                    v[0] += o.x; v[1] += o.y; v[2] += o.z; v[3] += o.w;
-                }
                 const int e0 = t * 32 + k * 8 + half * 4;
-                if (e0 < HD) *reinterpret_cast<uint2*>(out + e0) = make_uint2(pack2(v[0] * f, v[1] * f), pack2(v[2] * f, v[3] * f));
+                if (e0 < HD)
+                    *reinterpret_cast<uint2*>(to + e0) =
+                        make_uint2(pack2(a[t][k * 4] * f, a[t][k * 4 + 1] * f), pack2(a[t][k * 4 + 2] * f, a[t][k * 4 + 3] * f));
             }
     };
-    give(dk, 0);
-    sp_lds_barrier();
-    take(dk, 0, 0, g.scale);
-    sp_lds_barrier();
-    give(dv, 1);
-    sp_lds_barrier();
-    take(dv, 1, Hkv, 1.0f);
-}
-
-template <int HD, int KG>
-__global__ __launch_bounds__(BWD_WAVES * 64, 2) void attn_packed_bwd_kernel(BwdDev g, int dkv_groups) {
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem_bwd[];
-    if ((int)blockIdx.x < dkv_groups) dkv_group<HD, KG>(g, smem_bwd, blockIdx.x);
-    else dq_group<HD>(g, smem_bwd, blockIdx.x - dkv_groups);
-}
-
-template <int HD, int KG>
-hipError_t launch_bwd(hipStream_t st, const AttnBwdArgs& b, const PackedShape& a) {
-    constexpr int LDS = std::max(DqCfg<HD>::LDS, DkvCfg<HD, KG>::LDS);
-    static LdsLimitOnce lim;
-    hipError_t e = lim.set(reinterpret_cast<const void*>(attn_packed_bwd_kernel<HD, KG>), LDS);
-    if (e != hipSuccess) return e;
-    const float scale = 1.0f / sqrtf((float)HD);
-    const BwdDev g{b.qkv, b.dO, b.lse, b.delta, b.dqkv, a.cu, a.n, a.T, a.Hq, a.Hkv, a.causal, scale, scale * LOG2E};
-    const long kv = (((long)a.T / (32 * KG) + a.n) * a.Hkv + 7) / 8 * 8;         // ids of either kind begin on the first XCD
-    const bool two = a.Hq / a.Hkv % 2 == 0;
-    const long q = ((long)a.T / (two ? 128 : 256) + a.n) * (two ? a.Hq / 2 : a.Hq);
-    attn_packed_bwd_kernel<HD, KG><<<dim3((unsigned)(kv + q)), BWD_WAVES * 64, LDS, st>>>(g, (int)kv);
-    return hipGetLastError();
+    store(dk, out, g.scale);
+    store(dv, out + (size_t)Hkv * HD, 1.0f);
 }
 
 template <int HD>
-hipError_t launch_hd(hipStream_t st, const AttnBwdArgs& b, const PackedShape& a) {
-    return launch_bwd<HD, 4>(st, b, a);
+__global__ __launch_bounds__(BWD_WAVES * 64, 2) void attn_packed_bwd_kernel(BwdDev g, int dkv_groups) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem_bwd[];
+    if ((int)blockIdx.x < dkv_groups) dkv_group<HD>(g, smem_bwd, blockIdx.x);
+    else dq_group<HD>(g, smem_bwd, blockIdx.x - dkv_groups);
+}
+
+template <int HD>
+hipError_t launch_bwd(hipStream_t st, const AttnBwdArgs& b, const PackedShape& a) {
+    constexpr int LDS = std::max(DqCfg<HD>::LDS, DkvCfg<HD>::LDS);
+    static LdsLimitOnce lim;
+    hipError_t e = lim.set(reinterpret_cast<const void*>(attn_packed_bwd_kernel<HD>), LDS);
+    if (e != hipSuccess) return e;
+    const float scale = 1.0f / sqrtf((float)HD);
+    const BwdDev g{b.qkv, b.dO, b.lse, b.delta, b.dqkv, a.cu, a.n, a.T, a.Hq, a.Hkv, a.causal, scale, scale * LOG2E};
+    const long slots = (long)a.T / 128 + a.n;
+    const long kv = (slots * a.Hkv + 7) / 8 * 8;         // ids of either kind begin on the first XCD
+    attn_packed_bwd_kernel<HD><<<dim3((unsigned)(kv + slots * a.Hq)), BWD_WAVES * 64, LDS, st>>>(g, (int)kv);
+    return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t spk_launch_attention_packed_bwd(hipStream_t st, const AttnBwdArgs& b, const PackedShape& a) {
     switch (a.hd) {
-        case 64: return launch_hd<64>(st, b, a);
-        case 80: return launch_hd<80>(st, b, a);
-        case 128: return launch_hd<128>(st, b, a);
+        case 64: return launch_bwd<64>(st, b, a);
+        case 80: return launch_bwd<80>(st, b, a);
+        case 128: return launch_bwd<128>(st, b, a);
         default: return hipErrorInvalidValue;
     }
 }
