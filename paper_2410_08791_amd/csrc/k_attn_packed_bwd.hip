@@ -1,6 +1,6 @@
 // Backward of the attention over packed prompts: dq, dk, dv from q, k, v, dO, the forward's log-sum-exp and
 // delta = rowsum(dO * O), without atomics, in one launch of two kinds of work-groups that do not depend on one another:
-//   dk/dv -- a work-group owns 128 keys of one key/value head and walks the queries of every query head that shares it;
+//   dk/dv -- a work-group owns 32 KG keys of one key/value head and walks the queries of every query head that shares it;
 //   dq    -- a work-group owns 128 queries of one head and walks the keys.
 // P = exp(s - lse), dS = P (dP - delta), dP = dO V^T; layouts and tiles are those of k_attn_bwd.hip.
 //
@@ -280,26 +280,27 @@ __device__ __forceinline__ void dq_group(const BwdDev& g, unsigned char* smem, i
 }
 
 // ---------------------------------------------------------------------------------------------- dk, dv
-// Wave w takes the 32 keys of group w (one key per lane as the B operand of S = Q K^T and dP = dO V^T) against each tile of 32
-// queries.
-template <int HD>
+// Wave w takes the 32 keys of group w % KG (one key per lane as the B operand of S = Q K^T and dP = dO V^T) against the 32
+// queries of part w / KG of each tile; the parts' sums are added through LDS at the end.
+template <int HD, int KG>
 struct DkvCfg {
     typedef TokTile<HD> T;
-    static constexpr int ROWS = 32, KEYS = 128;
+    static constexpr int SUBS = BWD_WAVES / KG, ROWS = 32 * SUBS, KEYS = 32 * KG;
     static constexpr bool K_IN_LDS = HD == 128;       // K fragments would not fit beside the accumulators
     static constexpr int TILE = ROWS * T::ROWB, STAGE = 2 * TILE;
     static constexpr int KBYTES = K_IN_LDS ? KEYS * T::ROWB : 0;
-    static constexpr int LDS = STAGES<HD> * STAGE + KBYTES + STAGES<HD> * 2 * ROWS * 4;
-    static_assert(LDS <= 80 * 1024 && DqCfg<HD>::LDS <= 80 * 1024, "two work-groups fit a CU");
+    static constexpr int bytes(int stages) { return stages * STAGE + KBYTES + stages * 2 * ROWS * 4; }
+    static constexpr int STG = HD == 128 || bytes(3) > 80 * 1024 ? 2 : 3;
+    static constexpr int LDS = std::max(bytes(STG), SUBS > 1 ? (SUBS - 1) * KG * T::NMT * 16 * 256 : 0);
 };
 
-template <int HD>
+template <int HD, int KG>
 __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, int id) {
     typedef TokTile<HD> T;
-    typedef DkvCfg<HD> C;
-    constexpr int NK = T::NKS, NV = 2 * T::NMT, PF = 2;
+    typedef DkvCfg<HD, KG> C;
+    constexpr int NK = T::NKS, NV = 2 * T::NMT, PF = HD == 128 ? 2 : 3;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int l32 = lane & 31, half = lane >> 5;
+    const int l32 = lane & 31, half = lane >> 5, kg = wave % KG, sub = wave / KG;
     const int Hq = g.Hq, Hkv = g.Hkv, grp = Hq / Hkv, ld = (Hq + 2 * Hkv) * HD, ld_do = Hq * HD;
     const int slot = id / Hkv, kvh = near_heads(id - slot * Hkv, Hkv);
     const PackedBlock pb = packed_block<C::KEYS>(g.cu, g.n, g.T, slot);
@@ -307,18 +308,19 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
     if (pb.blk * C::KEYS >= len) return;
     // under a causal mask the first block has the most queries
     const int blk = g.causal ? (len - 1) / C::KEYS - pb.blk : pb.blk;
-    const int k0 = blk * C::KEYS, wk0 = k0 + wave * 32, kj = wk0 + l32;
+    const int k0 = blk * C::KEYS, wk0 = k0 + kg * 32, kj = wk0 + l32;
     const size_t tok0 = pb.row0;
     const bf16_t* kbase = g.qkv + tok0 * ld + (size_t)(Hq + kvh) * HD;
     const bf16_t* vbase = kbase + (size_t)Hkv * HD;
-    unsigned char* sKeys = smem + STAGES<HD> * C::STAGE;
-    float* rowvals = reinterpret_cast<float*>(smem + STAGES<HD> * C::STAGE + C::KBYTES);       // [stage][lse | delta][ROWS]
+    unsigned char* sKeys = smem + C::STG * C::STAGE;
+    float* rowvals = reinterpret_cast<float*>(smem + C::STG * C::STAGE + C::KBYTES);       // [stage][lse | delta][ROWS]
 
     // the tiles in walking order: (query head of the group, ROWS queries)
-    const int q_begin = g.causal ? k0 : 0;
+    const int q_begin = g.causal ? k0 / C::ROWS * C::ROWS : 0;
     const int per_head = (len - q_begin + C::ROWS - 1) / C::ROWS, n_tiles = grp * per_head;
     TileLoad<HD, C::ROWS> tl;
     tl.init(wave, lane);
+    constexpr int NR = (C::ROWS + 63) / 64;           // load instructions of a tile's row values
     int f_head = 0, f_q = q_begin;                    // of the tile fetched next
     auto fetch = [&](int stage) __attribute__((always_inline)) {
         const int h = kvh * grp + f_head;
@@ -330,7 +332,10 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
         if (wave < 2 && lane < C::ROWS) {
             const float* src = (wave ? g.delta : g.lse) + (size_t)h * g.T + tok0 + f_q;
             const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(src), 0, min(len - f_q, C::ROWS) * 4, 0x00020000);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void_ptr)(rowvals + (stage * 2 + wave) * C::ROWS), 4, lane * 4, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < NR; ++i)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void_ptr)(rowvals + (stage * 2 + wave) * C::ROWS + i * 64), 4,
+                                                         (i * 64 + lane) * 4, 0, 0, 0);
         }
 #endif
         f_q += C::ROWS;
@@ -357,35 +362,42 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
     for (int t = 0; t < T::NMT; ++t) { dk[t] = zeros(); dv[t] = zeros(); }
 
     fetch(0);
-    if (STAGES<HD> > 2 && n_tiles > 1) fetch(1);
-    int qs = q_begin;                                 // first query of the tile
+    if (C::STG > 2 && n_tiles > 1) fetch(1);
+    int qs = q_begin + sub * 32;                      // this wave's first query of the tile
     constexpr int NL = 2 * TileLoad<HD, C::ROWS>::NI; // a wave's loads of a tile, without the row values
     for (int tile = 0, stage = 0; tile < n_tiles; ++tile) {
         // the tile is there; everybody is done with the one before it, whose stage the next fetch takes
-        if (STAGES<HD> == 2 || tile + 1 == n_tiles) landed<0>();
-        else if (wave < 2) landed<NL + 1>();
+        if (C::STG == 2 || tile + 1 == n_tiles) landed<0>();
+        else if (wave < 2) landed<NL + NR>();
         else landed<NL>();
-        if (tile + STAGES<HD> - 1 < n_tiles) fetch(stage ? stage - 1 : STAGES<HD> - 1);
-        const int q_at = stage * C::STAGE;
-        const float* lrow = rowvals + stage * 2 * C::ROWS + half * 4;
-        // wave-uniform skips: every query of the tile precedes this wave's keys, no key exists
+        if (tile + C::STG - 1 < n_tiles) fetch(stage ? stage - 1 : C::STG - 1);
+        const int q_at = stage * C::STAGE + sub * 32 * T::ROWB;
+        const float* lrow = rowvals + stage * 2 * C::ROWS + sub * 32 + half * 4;
+        // wave-uniform skips: every query of the part precedes this wave's keys, none exists, no key exists
         if (!(qs >= len || wk0 >= len || (g.causal && qs + 31 < wk0))) {
             f32x16_t s, dp;
-            {
-                bf16x8_t qf[NK], kf[NK];
-                auto read = [&](int i) __attribute__((always_inline)) {
-                    qf[i] = at.row(smem, q_at, i, 0);
-                    if (C::K_IN_LDS) kf[i] = at.row(sKeys, wave * 32 * T::ROWB, i, 0);
-                };
+            u32x4_t pw[2], ds[2];
+            bf16x8_t qf[NK], kf[NK], df[NK], tv[NV], tk[NV];
+            float4 l4[4], d4[4];
+            auto read_s = [&](int i) __attribute__((always_inline)) {
+                qf[i] = at.row(smem, q_at, i, 0);
+                if (C::K_IN_LDS) kf[i] = at.row(sKeys, kg * 32 * T::ROWB, i, 0);
+            };
+            auto read_p = [&](int i) __attribute__((always_inline)) { df[i] = at.row(smem, q_at, i, C::TILE); };
+            auto read_v = [&](int i) __attribute__((always_inline)) { tv[i] = at.tr(smem, q_at, i % T::NMT, C::TILE + 16 * (i / T::NMT) * T::ROWB); };
+            auto read_k = [&](int i) __attribute__((always_inline)) { tk[i] = at.tr(smem, q_at, i % T::NMT, 16 * (i / T::NMT) * T::ROWB); };
+            // Four phases of MFMAs.  Each reads its fragments PF ahead, and with its last MFMAs the first ones of the next phase.
+            // S:
 #pragma unroll
-                for (int i = 0; i < PF; ++i) read(i);
+            for (int i = 0; i < PF; ++i) read_s(i);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < NK; ++i) {
+                if (i + PF < NK) read_s(i + PF);
+                else read_p(i + PF - NK);
+                if (i + 1 == NK) l4[0] = lds_f4(lrow);
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[i], C::K_IN_LDS ? kf[i] : kf_reg[C::K_IN_LDS ? 0 : i], i ? s : zeros(), 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int i = 0; i < NK; ++i) {
-                    if (i + PF < NK) read(i + PF);
-                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[i], C::K_IN_LDS ? kf[i] : kf_reg[C::K_IN_LDS ? 0 : i], i ? s : zeros(), 0, 0, 0);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
             }
             if ((g.causal && qs < wk0 + 31) || qs + 32 > len) {
                 // element e is query qs + 4 half + (e >> 2) * 8 + (e & 3)
@@ -396,124 +408,142 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
                     s[e] = q >= first && q < end ? s[e] : -INFINITY;
                 }
             }
-            // dP beside P, which takes the place of the scores; then dV beside dS; then dK
-            u32x4_t pw[2], ds[2];
-            {
-                bf16x8_t df[NK];
-                float4 l4[4];
-                l4[0] = lds_f4(lrow);                    // the others a step ahead of their use: registers are short here
+            // dP beside P, which takes the place of the scores; row values a step ahead of their use: registers are short here
 #pragma unroll
-                for (int i = 0; i < PF; ++i) df[i] = at.row(smem, q_at, i, C::TILE);
-                __builtin_amdgcn_sched_barrier(0);
+            for (int i = 0; i < NK; ++i) {
+                if (i + PF < NK) read_p(i + PF);
+                else read_v(i + PF - NK);
+                if (i + 1 == NK) d4[0] = lds_f4(lrow + C::ROWS);
 #pragma unroll
-                for (int i = 0; i < NK; ++i) {
-                    if (i + PF < NK) df[i + PF] = at.row(smem, q_at, i + PF, C::TILE);
+                for (int k = 1; k < 4; ++k)
+                    if (step_of(2 * k, NK, 8) == i + 1) l4[k] = lds_f4(lrow + k * 8);
+                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(df[i], vf[i], i ? dp : zeros(), 0, 0, 0);
 #pragma unroll
-                    for (int k = 1; k < 4; ++k)
-                        if (step_of(2 * k, NK, 8) == i + 1) l4[k] = lds_f4(lrow + k * 8);
-                    dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(df[i], vf[i], i ? dp : zeros(), 0, 0, 0);
-#pragma unroll
-                    for (int e = 8 * i / NK; e < 8 * (i + 1) / NK; ++e) {
-                        const float4 l = l4[e >> 1];
-                        const float a = __builtin_amdgcn_exp2f(fmaf(s[2 * e], g.scale_log2e, -LOG2E * ((e & 1) ? l.z : l.x)));
-                        const float b = __builtin_amdgcn_exp2f(fmaf(s[2 * e + 1], g.scale_log2e, -LOG2E * ((e & 1) ? l.w : l.y)));
-                        uint32_t w = pack2(a, b);
-                        asm volatile("" : "+v"(w));
-                        pw[e >> 2][e & 3] = w;
-                        s[2 * e] = a;
-                        s[2 * e + 1] = b;
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
+                for (int e = 8 * i / NK; e < 8 * (i + 1) / NK; ++e) {
+                    const float4 l = l4[e >> 1];
+                    const float a = __builtin_amdgcn_exp2f(fmaf(s[2 * e], g.scale_log2e, -LOG2E * ((e & 1) ? l.z : l.x)));
+                    const float b = __builtin_amdgcn_exp2f(fmaf(s[2 * e + 1], g.scale_log2e, -LOG2E * ((e & 1) ? l.w : l.y)));
+                    uint32_t w = pack2(a, b);
+                    asm volatile("" : "+v"(w));
+                    pw[e >> 2][e & 3] = w;
+                    s[2 * e] = a;
+                    s[2 * e + 1] = b;
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
-            {
-                bf16x8_t tf[NV];
-                float4 d4[4];
-                auto read = [&](int i) __attribute__((always_inline)) { tf[i] = at.tr(smem, q_at, i % T::NMT, C::TILE + 16 * (i / T::NMT) * T::ROWB); };
-                d4[0] = lds_f4(lrow + C::ROWS);
+            // dV beside dS
 #pragma unroll
-                for (int i = 0; i < PF; ++i) read(i);
-                __builtin_amdgcn_sched_barrier(0);
+            for (int i = 0; i < NV; ++i) {
+                if (i + PF < NV) read_v(i + PF);
+                else read_k(i + PF - NV);
 #pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    if (i + PF < NV) read(i + PF);
+                for (int k = 1; k < 4; ++k)
+                    if (step_of(2 * k, NV, 8) == i + 1) d4[k] = lds_f4(lrow + C::ROWS + k * 8);
+                dv[i % T::NMT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tv[i], __builtin_bit_cast(bf16x8_t, pw[i / T::NMT]), dv[i % T::NMT], 0, 0, 0);
 #pragma unroll
-                    for (int k = 1; k < 4; ++k)
-                        if (step_of(2 * k, NV, 8) == i + 1) d4[k] = lds_f4(lrow + C::ROWS + k * 8);
-                    dv[i % T::NMT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tf[i], __builtin_bit_cast(bf16x8_t, pw[i / T::NMT]), dv[i % T::NMT], 0, 0, 0);
-#pragma unroll
-                    for (int e = 8 * i / NV; e < 8 * (i + 1) / NV; ++e) {
-                        const float4 d = d4[e >> 1];
-                        uint32_t w = pack2(s[2 * e] * (dp[2 * e] - ((e & 1) ? d.z : d.x)), s[2 * e + 1] * (dp[2 * e + 1] - ((e & 1) ? d.w : d.y)));
-                        asm volatile("" : "+v"(w));
-                        ds[e >> 2][e & 3] = w;
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
+                for (int e = 8 * i / NV; e < 8 * (i + 1) / NV; ++e) {
+                    const float4 d = d4[e >> 1];
+                    uint32_t w = pack2(s[2 * e] * (dp[2 * e] - ((e & 1) ? d.z : d.x)), s[2 * e + 1] * (dp[2 * e + 1] - ((e & 1) ? d.w : d.y)));
+                    asm volatile("" : "+v"(w));
+                    ds[e >> 2][e & 3] = w;
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
-            {
-                bf16x8_t tf[NV];
-                auto read = [&](int i) __attribute__((always_inline)) { tf[i] = at.tr(smem, q_at, i % T::NMT, 16 * (i / T::NMT) * T::ROWB); };
+            // dK
 #pragma unroll
-                for (int i = 0; i < PF; ++i) read(i);
+            for (int i = 0; i < NV; ++i) {
+                if (i + PF < NV) read_k(i + PF);
+                dk[i % T::NMT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tk[i], __builtin_bit_cast(bf16x8_t, ds[i / T::NMT]), dk[i % T::NMT], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    if (i + PF < NV) read(i + PF);
-                    dk[i % T::NMT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tf[i], __builtin_bit_cast(bf16x8_t, ds[i / T::NMT]), dk[i % T::NMT], 0, 0, 0);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
             }
         }
         qs += C::ROWS;
-        if (qs >= len) qs = q_begin;
-        stage = stage + 1 == STAGES<HD> ? 0 : stage + 1;
+        if (qs - sub * 32 >= len) qs = q_begin + sub * 32;
+        stage = stage + 1 == C::STG ? 0 : stage + 1;
     }
-    if (kj >= len) return;
-    bf16_t* out = g.dqkv + (tok0 + kj) * ld + (size_t)(Hq + kvh) * HD;
-    auto store = [&](const f32x16_t* a, bf16_t* to, float f) {
+    // The parts' sums meet in LDS: dK in part 0, dV in the next, added in the order of the parts.
+    if (C::SUBS > 1) landed<0>();
+    float4* x = reinterpret_cast<float4*>(smem) + lane;
+    auto place = [&](int s, int owner) { return ((s < owner ? s : s - 1) * KG + kg) * (T::NMT * 4 * 64); };
+    auto give = [&](const f32x16_t* a, int owner) __attribute__((always_inline)) {
+        if (sub == owner) return;
+#pragma unroll
+        for (int t = 0; t < T::NMT; ++t)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                x[place(sub, owner) + (t * 4 + k) * 64] = make_float4(a[t][k * 4], a[t][k * 4 + 1], a[t][k * 4 + 2], a[t][k * 4 + 3]);
+    };
+    auto take = [&](const f32x16_t* a, int owner, int col, float f) __attribute__((always_inline)) {
+        if (sub != owner || kj >= len) return;
+        bf16_t* out = g.dqkv + (tok0 + kj) * ld + (size_t)(Hq + col + kvh) * HD;
 #pragma unroll
         for (int t = 0; t < T::NMT; ++t)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
+                float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int s = 0; s < C::SUBS; ++s) {
+                    const float4 o = s == owner ? make_float4(a[t][k * 4], a[t][k * 4 + 1], a[t][k * 4 + 2], a[t][k * 4 + 3])
+                                                : x[place(s, owner) + (t * 4 + k) * 64];
+                    v[0] += o.x; v[1] += o.y; v[2] += o.z; v[3] += o.w;
+                }
                 const int e0 = t * 32 + k * 8 + half * 4;
-                if (e0 < HD)
-                    *reinterpret_cast<uint2*>(to + e0) =
-                        make_uint2(pack2(a[t][k * 4] * f, a[t][k * 4 + 1] * f), pack2(a[t][k * 4 + 2] * f, a[t][k * 4 + 3] * f));
+                if (e0 < HD) *reinterpret_cast<uint2*>(out + e0) = make_uint2(pack2(v[0] * f, v[1] * f), pack2(v[2] * f, v[3] * f));
             }
     };
-    store(dk, out, g.scale);
-    store(dv, out + (size_t)Hkv * HD, 1.0f);
+    if (C::SUBS > 1) { give(dk, 0); sp_lds_barrier(); }
+    take(dk, 0, 0, g.scale);
+    if (C::SUBS > 1) { sp_lds_barrier(); give(dv, 1); sp_lds_barrier(); }
+    take(dv, C::SUBS > 1 ? 1 : 0, Hkv, 1.0f);
 }
 
-template <int HD>
+template <int HD, int KG>
 __global__ __launch_bounds__(BWD_WAVES * 64, 2) void attn_packed_bwd_kernel(BwdDev g, int dkv_groups) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem_bwd[];
-    if ((int)blockIdx.x < dkv_groups) dkv_group<HD>(g, smem_bwd, blockIdx.x);
+    if ((int)blockIdx.x < dkv_groups) dkv_group<HD, KG>(g, smem_bwd, blockIdx.x);
     else dq_group<HD>(g, smem_bwd, blockIdx.x - dkv_groups);
 }
 
-template <int HD>
+template <int HD, int KG>
 hipError_t launch_bwd(hipStream_t st, const AttnBwdArgs& b, const PackedShape& a) {
-    constexpr int LDS = std::max(DqCfg<HD>::LDS, DkvCfg<HD>::LDS);
+    constexpr int LDS = std::max(DqCfg<HD>::LDS, DkvCfg<HD, KG>::LDS);
     static LdsLimitOnce lim;
-    hipError_t e = lim.set(reinterpret_cast<const void*>(attn_packed_bwd_kernel<HD>), LDS);
+    hipError_t e = lim.set(reinterpret_cast<const void*>(attn_packed_bwd_kernel<HD, KG>), LDS);
     if (e != hipSuccess) return e;
     const float scale = 1.0f / sqrtf((float)HD);
     const BwdDev g{b.qkv, b.dO, b.lse, b.delta, b.dqkv, a.cu, a.n, a.T, a.Hq, a.Hkv, a.causal, scale, scale * LOG2E};
     const long slots = (long)a.T / 128 + a.n;
-    const long kv = (slots * a.Hkv + 7) / 8 * 8;         // ids of either kind begin on the first XCD
-    attn_packed_bwd_kernel<HD><<<dim3((unsigned)(kv + slots * a.Hq)), BWD_WAVES * 64, LDS, st>>>(g, (int)kv);
+    const long kv = (((long)a.T / (32 * KG) + a.n) * a.Hkv + 7) / 8 * 8;         // ids of either kind begin on the first XCD
+    attn_packed_bwd_kernel<HD, KG><<<dim3((unsigned)(kv + slots * a.Hq)), BWD_WAVES * 64, LDS, st>>>(g, (int)kv);
     return hipGetLastError();
+}
+
+// Keys of a dk/dv work-group.  Its chain is the queries of all heads that share them, 32 at a time: with 128 keys per group that
+// is what a batch of few groups waits for, with fewer the waves share out the queries and the chain is a half or a quarter.
+// But each group loads all queries, and at head_dim 128 only one of it fits a CU then.  us for 128, 64, 32 keys (groups of 128
+// keys in brackets):
+//   head_dim 64:  900 + 200 tokens, 8/4 heads (40) 53.5 30.3 21.4;  3 x 2000, 8/2 (98) 211 115 85;  3000, 8/8 (192) 84 58 69;
+//                 8 x 512, 16/16 (640) 45.3 44.7 55.3;  12 x 300, 32/32 (1280) 58.7 61.2 81.0
+//   head_dim 80:  1500 + 300, 8/2 (32) 161 91 58;  6 x 700, 32/8 (304) 125 97 149;  8 x 577, 16/16 (704) 60.9 63.9 112.6; 4 x 1000,
+//                 8/8 (280), where the chain is one head, 42.5 45.1 61.7
+//   head_dim 128: 3 x 2000, 8/2 (98) 274 155 165;  3000, 8/8 (192) 118 108 132;  6 x 700, 32/8 (304) 158 161 201
+template <int HD>
+hipError_t launch_hd(hipStream_t st, const AttnBwdArgs& b, const PackedShape& a) {
+    const long groups = ((long)a.T / 128 + a.n) * a.Hkv;
+    if (HD == 128) return groups <= 192 ? launch_bwd<HD, 2>(st, b, a) : launch_bwd<HD, 4>(st, b, a);
+    if constexpr (HD != 128)
+        if (groups <= (HD == 64 ? 128 : 64)) return launch_bwd<HD, 1>(st, b, a);
+    if (HD == 64 ? groups <= 640 : groups <= 512 && a.Hq > a.Hkv) return launch_bwd<HD, 2>(st, b, a);
+    return launch_bwd<HD, 4>(st, b, a);
 }
 
 }  // namespace
 
 hipError_t spk_launch_attention_packed_bwd(hipStream_t st, const AttnBwdArgs& b, const PackedShape& a) {
     switch (a.hd) {
-        case 64: return launch_bwd<64>(st, b, a);
-        case 80: return launch_bwd<80>(st, b, a);
-        case 128: return launch_bwd<128>(st, b, a);
+        case 64: return launch_hd<64>(st, b, a);
+        case 80: return launch_hd<80>(st, b, a);
+        case 128: return launch_hd<128>(st, b, a);
         default: return hipErrorInvalidValue;
     }
 }
