@@ -299,6 +299,176 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void attn_packed_kernel
     }
 }
 
+// The same for batches of few blocks: a work-group has 32 queries of one head and its four waves share out the keys, wave w
+// the steps of 32 keys w, w + 4, ...  A wave loads its steps into two LDS buffers of its own and waits for nobody; at the
+// end the waves' outputs, sums and maxima meet in LDS and are added in wave order.  What bounds such a batch is the chain
+// of one wave, which is a quarter as long so.
+template <int HD>
+struct SplitCfg {
+    typedef AttnCfg<HD, 1> C;
+    static constexpr int WAVES = 4, TILE = 32 * C::ROWB, BUF = 2 * TILE;        // K rows, then V rows
+    static constexpr int NI = BUF / 1024;                                      // load instructions of a step
+    static constexpr int MERGE = WAVES * (C::NMT * 16 + 2) * 64 * 4, LOOP = WAVES * 2 * BUF;
+    static constexpr int LDS = MERGE > LOOP ? MERGE : LOOP;
+    static_assert(TILE % 1024 == 0 && LDS <= 160 * 1024, "whole load instructions, and they fit the LDS");
+};
+
+template <int HD>
+__global__ __launch_bounds__(256, 1) void attn_packed_split_kernel(const bf16_t* __restrict__ qkv, const int* __restrict__ cu,
+                                                                 bf16_t* __restrict__ o, float* __restrict__ lse, int n, int T, int Hq,
+                                                                 int Hkv, int causal, float scale_log2e) {
+    typedef SplitCfg<HD> G;
+    typedef typename G::C C;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem_split[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l32 = lane & 31, half = lane >> 5;
+    const int slot = blockIdx.x / Hq, hi = blockIdx.x - slot * Hq;
+    const int h = Hq & 7 ? hi : (hi & 7) * (Hq >> 3) + (hi >> 3);
+    const PackedBlock pb = packed_block<32>(cu, n, T, slot);
+    const int len = pb.len, q0 = pb.blk * 32, qi = q0 + l32, ld = (Hq + 2 * Hkv) * HD;
+    if (q0 >= len) return;
+    const size_t tok0 = pb.row0;
+    [[maybe_unused]] const bf16_t* kbase = qkv + tok0 * ld + (size_t)(Hq + h / (Hq / Hkv)) * HD;
+    const int steps = ((causal ? min(len, q0 + 32) : len) + 31) / 32;
+    auto issue = [&](int i) __attribute__((always_inline)) {
+#if defined(__HIP_DEVICE_COMPILE__)
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(kbase + (size_t)i * 32 * ld), 0, min(len - i * 32, 32) * ld * 2,
+                                                            0x00020000);
+#pragma unroll
+        for (int k = 0; k < G::NI; ++k) {
+            const bool isv = k * 1024 >= G::TILE;
+            const int rel = k * 1024 + lane * 16 - (isv ? G::TILE : 0), row = rel / C::ROWB, pos = (rel % C::ROWB) >> 4;
+            const int c = isv ? pos ^ (C::v_swz(row) << 2) : pos ^ C::k_swz(row);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void_ptr)(smem_split + (wave * 2 + ((i >> 2) & 1)) * G::BUF + k * 1024), 16,
+                                                     c < C::CPR ? (row * ld + (isv ? Hkv * HD : 0) + c * 8) * 2 : -1, 0, 0, 0);
+        }
+#endif
+    };
+    if (wave < steps) issue(wave);
+    bf16x8_t qf[C::NKS];
+    {
+        const bf16_t* qp = qkv + (tok0 + min(qi, len - 1)) * ld + h * HD + half * 8;
+#pragma unroll
+        for (int ks = 0; ks < C::NKS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8_t*>(qp + ks * 16);
+    }
+    const int rowv = half * 4 + ((lane & 15) >> 2);
+    f32x16_t acc[C::NMT];
+#pragma unroll
+    for (int t = 0; t < C::NMT; ++t) acc[t] = zeros();
+    float m_run = -3.402823466e38f, l_run = 0.f;       // finite: a wave may hold no key that a query sees
+    for (int i = wave; i < steps; i += G::WAVES) {
+        // the last user of the other buffer has read it: every fragment went into an MFMA
+        if (i + G::WAVES < steps) {
+            issue(i + G::WAVES);
+            __builtin_amdgcn_s_waitcnt(sp_waitcnt(G::NI, 15));
+        } else {
+            __builtin_amdgcn_s_waitcnt(sp_waitcnt(0, 15));
+        }
+        asm volatile("" ::: "memory");
+        const unsigned char* sK = smem_split + (wave * 2 + ((i >> 2) & 1)) * G::BUF;
+        bf16x8_t kf[C::NKS];
+#pragma unroll
+        for (int ks = 0; ks < C::NKS; ++ks) kf[ks] = lds_frag(sK + l32 * C::ROWB + (((2 * ks + half) ^ C::k_swz(l32)) << 4));
+        s16x4_t lo[2 * C::NMT], hi4[2 * C::NMT];
+#pragma unroll
+        for (int k = 0; k < 2 * C::NMT; ++k) {
+            const int mt = k % C::NMT, j = k / C::NMT;
+            const unsigned char* vp = sK + G::TILE + (rowv + 16 * j) * C::ROWB + ((mt ^ C::v_swz(rowv)) << 6) + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+            lo[k] = sp_tr_read((lds_s16x4_ptr)(vp));
+            hi4[k] = sp_tr_read((lds_s16x4_ptr)(vp + 8 * C::ROWB));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        f32x16_t s;
+#pragma unroll
+        for (int ks = 0; ks < C::NKS; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[ks], ks ? s : zeros(), 0, 0, 0);
+        if (i * 32 + 32 > len || (causal && i * 32 + 31 > q0)) {
+            const int last = min(len - 1, causal ? qi : len - 1) - i * 32 - 4 * half;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = (e >> 2) * 8 + (e & 3) <= last ? s[e] : -INFINITY;
+        }
+        float mx = s[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
+        const float top = half_max(mx);
+        const bool move = (top - m_run) * scale_log2e > 8.0f;
+        const float m_new = move ? top : m_run;
+        float alpha = move ? __builtin_amdgcn_exp2f((m_run - m_new) * scale_log2e) : 1.0f;
+        m_run = m_new;
+        if (__any(move)) {
+            asm volatile("" : "+v"(alpha));
+            l_run *= alpha;
+#pragma unroll
+            for (int t = 0; t < C::NMT; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[t][e] *= alpha;
+        }
+        u32x4_t p[2];
+        const float m_scaled = m_new * scale_log2e;
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float v = __builtin_amdgcn_exp2f(fmaf(s[2 * e], scale_log2e, -m_scaled));
+            const float w = __builtin_amdgcn_exp2f(fmaf(s[2 * e + 1], scale_log2e, -m_scaled));
+            sum += v + w;
+            p[e >> 2][e & 3] = __builtin_bit_cast(uint32_t, bf16x2_t{(__bf16)v, (__bf16)w});
+        }
+        l_run += sum;
+#pragma unroll
+        for (int k = 0; k < 2 * C::NMT; ++k) {
+            const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, s16x8_t{lo[k][0], lo[k][1], lo[k][2], lo[k][3], hi4[k][0], hi4[k][1], hi4[k][2], hi4[k][3]});
+            acc[k % C::NMT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8_t, p[k / C::NMT]), acc[k % C::NMT], 0, 0, 0);
+        }
+    }
+    const float l = l_run + __shfl_xor(l_run, 32, 64);
+    __syncthreads();                          // the buffers are free
+    float4* rows = reinterpret_cast<float4*>(smem_split);                        // [wave][group of four rows][lane]
+    float* ml = reinterpret_cast<float*>(smem_split) + G::WAVES * C::NMT * 16 * 64;      // [wave][maximum, sum][lane]
+#pragma unroll
+    for (int t = 0; t < C::NMT; ++t)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            rows[((wave * C::NMT + t) * 4 + k) * 64 + lane] = make_float4(acc[t][k * 4], acc[t][k * 4 + 1], acc[t][k * 4 + 2], acc[t][k * 4 + 3]);
+    ml[(wave * 2) * 64 + lane] = m_run;
+    ml[(wave * 2 + 1) * 64 + lane] = l;
+    __syncthreads();
+    float M = ml[lane], f[G::WAVES], L = 0.f;
+#pragma unroll
+    for (int w = 1; w < G::WAVES; ++w) M = fmaxf(M, ml[w * 2 * 64 + lane]);
+#pragma unroll
+    for (int w = 0; w < G::WAVES; ++w) {
+        f[w] = __builtin_amdgcn_exp2f((ml[w * 2 * 64 + lane] - M) * scale_log2e);
+        L = fmaf(f[w], ml[(w * 2 + 1) * 64 + lane], L);
+    }
+    if (qi >= len) return;
+    const float inv = 1.0f / L;
+    bf16_t* op = o + (tok0 + qi) * (size_t)(Hq * HD) + h * HD;
+#pragma unroll
+    for (int i = 0; i < C::NMT; ++i) {
+        const int grp = wave + G::WAVES * i, e0 = grp * 8 + half * 4;            // group of eight rows, four a lane
+        if (e0 >= HD) continue;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < G::WAVES; ++w) {
+            const float4 r = rows[(w * C::NMT * 4 + grp) * 64 + lane];
+            v[0] = fmaf(f[w], r.x, v[0]); v[1] = fmaf(f[w], r.y, v[1]); v[2] = fmaf(f[w], r.z, v[2]); v[3] = fmaf(f[w], r.w, v[3]);
+        }
+        *reinterpret_cast<uint2*>(op + e0) = make_uint2(pack_bf2(v[0] * inv, v[1] * inv), pack_bf2(v[2] * inv, v[3] * inv));
+    }
+    if (lse && wave == 0 && half == 0) lse[(size_t)h * T + tok0 + qi] = M * scale_log2e * 0.69314718055994530942f + logf(L);
+}
+
+template <int HD>
+hipError_t launch_split(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* lse, const PackedShape& a) {
+    typedef SplitCfg<HD> G;
+    static LdsLimitOnce lds_limit;
+    hipError_t e = lds_limit.set(reinterpret_cast<const void*>(attn_packed_split_kernel<HD>), G::LDS);
+    if (e != hipSuccess) return e;
+    const long slots = (long)a.T / 32 + a.n;
+    attn_packed_split_kernel<HD><<<dim3((unsigned)(slots * a.Hq)), 256, G::LDS, st>>>(qkv, a.cu, o, lse, a.n, a.T, a.Hq, a.Hkv, a.causal,
+                                                                                     1.4426950408889634f / sqrtf((float)HD));
+    return hipGetLastError();
+}
+
 template <int HD, int NW>
 hipError_t launch_packed(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* lse, const PackedShape& a) {
     typedef PackedCfg<HD, NW> G;
@@ -311,9 +481,19 @@ hipError_t launch_packed(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* ls
     return hipGetLastError();
 }
 
+// Shared-out keys while the 32-query groups are few: one per CU at head_dim 80, two else, and some more where the sequences are
+// long on average (their first blocks have few keys under a causal mask).  us, 128 queries and 32 (groups of 32):
+//   head_dim 64:  5 prompts of 1 to 128 tokens, 4 heads (56) 5.4 4.2;  3000 tokens, 4 heads (376) 39.7 19.8;  2 x 1000, 16 heads
+//                 (1024) 17.9 16.4;  30 x 100, 8 heads (984) 6.7 8.2;  3000, 16 heads (1504) 43.1 43.5
+//   head_dim 80:  257 tokens, 16 heads (144) 9.2 6.2;  4 x 257 (576) 9.6 16.3
+//   head_dim 128: 2 x 1000, 8 heads (512) 23.6 16.1;  3000, 8 heads (752) 61.2 47.0;  3 x 500, 16 heads (784) 15.1 18.8;
+//                 3000, 16 heads (1504) 64.2 82.0
 template <int HD>
 hipError_t launch_hd(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* lse, const PackedShape& a) {
-    return launch_packed<HD, 4>(st, qkv, o, lse, a);
+    const long groups = ((long)a.T / 32 + a.n) * a.Hq;
+    const bool lengthy = a.T / a.n >= 1000;
+    const long most = HD == 80 ? 256 : !lengthy ? 512 : HD == 64 ? 1024 : 768;
+    return groups <= most ? launch_split<HD>(st, qkv, o, lse, a) : launch_packed<HD, 4>(st, qkv, o, lse, a);
 }
 
 }  // namespace
