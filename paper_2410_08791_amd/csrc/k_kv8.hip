@@ -21,51 +21,41 @@ typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ float exp2_bits(int biased) { return __uint_as_float((uint32_t)biased << 23); }
 
 // ---------------------------------------------------------------------------------------------- append
-// A run is a maximal row of tokens with consecutive slots inside one block.  One wave writes the keys, another the values
-// of one block and head, run after run in the order of the rows, and nobody else touches them: a row whose block
-// occurs in the 64 rows before it leaves the block to the wave that met it first.  The wave holds the whole run in registers (64 tokens of 128: 64
-// VGPRs), so it is read once, between the largest value and the coding.  Lane (rg, c) has the block positions
-// rg * TPL .. rg * TPL + TPL - 1 of the elements 8 c .. 8 c + 7: a row of keys leaves in pieces of 8 bytes, and the
-// transposition that the value layout needs happens inside the lane.
+// A run is a maximal row of tokens with consecutive slots inside one block.  The keys, and apart from them the values, of one
+// block and head are written by one wave or work-group, run after run in the order of the rows, and nobody else touches
+// them: a row whose block occurs in the 64 rows before it leaves the block to whoever met it first.
+// NL lanes work a run in parts of GROUPS * TPL positions: lane (rg, ch) has TPL neighbouring positions of the elements
+// 8 ch .. 8 ch + 7, so that a row of keys leaves in pieces of 8 bytes, and the transposition that the value layout needs
+// happens inside the lane.  Between the largest value and the coding a run of one part stays in registers; a longer one is
+// read again, out of the cache.
 // HBM-bound for prompts (4 bytes read and 2 written per token, head and element), latency-bound for single tokens: their
 // block is read again only where its scale grows.
-// What a run needs to know comes from the slots alone: `range` tokens per wave are looked at for the beginning of a run.
-template <int HD, int BS>
-__global__ __launch_bounds__(256) void kv8_append_kernel(const bf16_t* __restrict__ qkv, const int* __restrict__ slots, int T, int range,
-                                                         int Hq, Kv8Cache c) {
-    constexpr int LPR = HD / 8, RPI = 64 / LPR, TPL = BS / RPI;      // lanes per row, rows per instruction, positions per lane
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int rg = lane / LPR, ch = lane % LPR;
-    const int Hkv = c.Hkv, ld = (Hq + 2 * Hkv) * HD;
-    const int isv = blockIdx.y & 1, h = blockIdx.y >> 1;
-    const int limit = c.blocks * BS;
-    const int begin = ((int)blockIdx.x * 4 + wave) * range;         // T <= 2^30
-    if (begin >= T) return;
-    auto slot_at = [&](int row) { return row >= 0 && row < T ? slots[row] : -1; };
-    const int before = slot_at(begin - 64 + lane), from = slot_at(begin + lane);
-    for (int i = 0; i < range && begin + i < T; ++i) {
-        int t = begin + i;
-        int s = __builtin_amdgcn_readfirstlane(__shfl(from, i, 64));
-        if (s < 0 || s >= limit) continue;
-        const int block = s / BS;
-        auto here = [&](int slot) { return slot >= 0 && slot / BS == block; };
-        if (__any(lane >= i ? here(before) : here(from))) continue;      // one of the 64 rows in front of t
-        for (;;) {
-        const int off = s % BS;
-        // the run's length: its slots follow one another up to the end of the block
-        const bool in = lane < BS - off && slot_at(t + lane) == s + lane;
-        const unsigned long long miss = ~__ballot(in);
-        const int m = miss ? __builtin_ctzll(miss) : 64;
-        const size_t bh = (size_t)block * Hkv + h;
-        const bf16_t* src = qkv + (size_t)t * ld + (size_t)(Hq + isv * Hkv + h) * HD + ch * 8;
-        u32x4_t x[TPL];
-        uint32_t big = 0;
+
+// m tokens from row t on go to the positions off .. of a block.  NL == 256: by the whole work-group, `tops` its four words of LDS.
+template <int HD, int BS, int NL>
+__device__ __forceinline__ void store_run(const bf16_t* __restrict__ qkv, int ld, int Hq, const Kv8Cache& c, int h, int isv, int t, int m,
+                                          int block, int off, int* tops) {
+    constexpr int LPR = HD / 8, GROUPS = NL / LPR;                          // lanes per row, rows at a time
+    constexpr int TPL = BS >= 4 * GROUPS ? 4 : BS > GROUPS ? BS / GROUPS : 1, PART = GROUPS * TPL;
+    const int id = NL == 64 ? threadIdx.x & 63 : threadIdx.x, lane = threadIdx.x & 63;
+    const int rg = id / LPR, ch = id % LPR;
+    const size_t bh = (size_t)block * c.Hkv + h;
+    const bf16_t* src = qkv + (size_t)t * ld + (size_t)(Hq + isv * c.Hkv + h) * HD + ch * 8;
+    float* sp = c.scales + bh * 2 + isv;
+    const int e_old = off ? min(max((int)((__float_as_uint(*sp) >> 23) & 255), 1), 253) : 0;
+    u32x4_t x[TPL];
+    const int from = off / PART, to = (off + m - 1) / PART;      // parts that hold new tokens
+    auto load = [&](int part) {
 #pragma unroll
         for (int i = 0; i < TPL; ++i) {
-            const int p = rg * TPL + i - off;                        // token of the run
+            const int p = part * PART + rg * TPL + i - off;      // token of the run
             x[i] = u32x4_t{0, 0, 0, 0};
             if (p >= 0 && p < m) x[i] = *reinterpret_cast<const u32x4_t*>(src + (size_t)p * ld);
         }
+    };
+    uint32_t big = 0;
+    for (int part = from; part <= to; ++part) {
+        load(part);
 #pragma unroll
         for (int i = 0; i < TPL; ++i)
 #pragma unroll
@@ -73,12 +63,24 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(const bf16_t* __restric
                 const u16x2_t a = __builtin_bit_cast(u16x2_t, x[i][k] & 0x7fff7fffu);
                 big = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, big), a));
             }
-        int top = max(big & 0xffff, big >> 16);
+    }
+    auto over_lanes = [&](int v) {
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o, 64));
-        const bool odd = top >= 0x7f80;                              // infinities or NaN among them: stored as NaN, the scale is the others'
-        if (odd) {
-            top = 0;
+        for (int o = 32; o > 0; o >>= 1) v = max(v, __shfl_xor(v, o, 64));
+        if (NL > 64) {
+            __syncthreads();
+            if (lane == 0) tops[threadIdx.x >> 6] = v;
+            __syncthreads();
+            v = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+        }
+        return v;
+    };
+    int top = over_lanes(max((int)(big & 0xffff), (int)(big >> 16)));
+    const bool odd = top >= 0x7f80;                              // infinities or NaN among them: stored as NaN, the scale is the others'
+    if (odd) {
+        top = 0;
+        for (int part = from; part <= to; ++part) {
+            load(part);
 #pragma unroll
             for (int i = 0; i < TPL; ++i)
 #pragma unroll
@@ -86,40 +88,41 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(const bf16_t* __restric
                     const int lo = x[i][k] & 0x7fff, hi = (x[i][k] >> 16) & 0x7fff;
                     top = max(top, max(lo < 0x7f80 ? lo : 0, hi < 0x7f80 ? hi : 0));
                 }
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o, 64));
         }
-        // biased exponent of the scale: 1.75 * 2^8 is the largest code
-        int e = max((top >> 7) - 8 + ((top & 127) > 96 ? 1 : 0), 1);
-        float* sp = c.scales + bh * 2 + isv;
-        const int e_old = off ? min(max((int)((__float_as_uint(*sp) >> 23) & 255), 1), 253) : 0;
-        e = max(e, e_old);
-        const bool grow = off && e > e_old;
-        const float inv = exp2_bits(254 - e), shift = exp2_bits(max(127 + e_old - e, 0));
-        if (lane == 0 && e != e_old) *sp = exp2_bits(e);
-        auto code4 = [&](uint32_t w0, uint32_t w1) {                 // four bf16 values
-            int r = __builtin_amdgcn_cvt_pk_fp8_f32(bf_lo(w0) * inv, bf_hi(w0) * inv, 0, false);
-            r = __builtin_amdgcn_cvt_pk_fp8_f32(bf_lo(w1) * inv, bf_hi(w1) * inv, r, true);
-            if (odd) {
-                const uint32_t w[2] = {w0, w1};
+        top = over_lanes(top);
+    }
+    // biased exponent of the scale: 1.75 * 2^8 is the largest code
+    int e = max((top >> 7) - 8 + ((top & 127) > 96 ? 1 : 0), 1);
+    e = max(e, e_old);
+    const bool grow = off && e > e_old;
+    const float inv = exp2_bits(254 - e), shift = exp2_bits(max(127 + e_old - e, 0));
+    if (id == 0 && e != e_old) *sp = exp2_bits(e);               // everybody has read the old one: the work-group met in over_lanes
+    auto code4 = [&](uint32_t w0, uint32_t w1) {                 // four bf16 values
+        int r = __builtin_amdgcn_cvt_pk_fp8_f32(bf_lo(w0) * inv, bf_hi(w0) * inv, 0, false);
+        r = __builtin_amdgcn_cvt_pk_fp8_f32(bf_lo(w1) * inv, bf_hi(w1) * inv, r, true);
+        if (odd) {
+            const uint32_t w[2] = {w0, w1};
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint32_t v = w[k >> 1] >> (16 * (k & 1));
-                    if ((v & 0x7fff) >= 0x7f80) r = (r & ~(255u << (8 * k))) | ((127u | (v >> 8 & 128u)) << (8 * k));
-                }
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t v = w[k >> 1] >> (16 * (k & 1));
+                if ((v & 0x7fff) >= 0x7f80) r = (r & ~(255u << (8 * k))) | ((127u | (v >> 8 & 128u)) << (8 * k));
             }
-            return (uint32_t)r;
-        };
-        auto recode4 = [&](uint32_t w) {
-            const f32x2_t a = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
-            int r = __builtin_amdgcn_cvt_pk_fp8_f32(a.x * shift, a.y * shift, 0, false);
-            return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(b.x * shift, b.y * shift, r, true);
-        };
+        }
+        return (uint32_t)r;
+    };
+    auto recode4 = [&](uint32_t w) {
+        const f32x2_t a = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+        int r = __builtin_amdgcn_cvt_pk_fp8_f32(a.x * shift, a.y * shift, 0, false);
+        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(b.x * shift, b.y * shift, r, true);
+    };
+    for (int part = grow ? 0 : from; part <= to; ++part) {
+        if (from != to || grow) load(part);
+        const int p0 = part * PART + rg * TPL;
         if (!isv) {
             uint8_t* dst = c.k8 + bh * (BS * HD) + ch * 8;
 #pragma unroll
             for (int i = 0; i < TPL; ++i) {
-                const int p = rg * TPL + i;
+                const int p = p0 + i;
                 uint32_t* d = reinterpret_cast<uint32_t*>(dst + p * HD);
                 if (p >= off && p < off + m) {
                     *reinterpret_cast<uint2*>(d) = make_uint2(code4(x[i][0], x[i][1]), code4(x[i][2], x[i][3]));
@@ -128,61 +131,110 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(const bf16_t* __restric
                     *reinterpret_cast<uint2*>(d) = make_uint2(recode4(o.x), recode4(o.y));
                 }
             }
-        } else {
-            uint8_t* dst = c.v8 + bh * (BS * HD) + (size_t)ch * 8 * BS + rg * TPL;
-            uint32_t y[TPL][2];
+            continue;
+        }
+        uint8_t* dst = c.v8 + bh * (BS * HD) + (size_t)ch * 8 * BS + p0;
+        uint32_t y[TPL][2];
 #pragma unroll
-            for (int i = 0; i < TPL; ++i) { y[i][0] = code4(x[i][0], x[i][1]); y[i][1] = code4(x[i][2], x[i][3]); }
-            const int p0 = rg * TPL;
-            const bool whole = p0 >= off && p0 + TPL <= off + m;
-            const bool some = p0 < off + m && p0 + TPL > (grow ? 0 : off);
-            if (whole) {
+        for (int i = 0; i < TPL; ++i) { y[i][0] = code4(x[i][0], x[i][1]); y[i][1] = code4(x[i][2], x[i][3]); }
+        if (p0 >= off && p0 + TPL <= off + m) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    uint32_t w[(TPL + 3) / 4] = {};
+            for (int k = 0; k < 8; ++k) {
+                uint32_t w = 0;
 #pragma unroll
-                    for (int i = 0; i < TPL; ++i) w[i / 4] |= ((y[i][k >> 2] >> (8 * (k & 3))) & 255u) << (8 * (i & 3));
-                    if constexpr (TPL == 16) *reinterpret_cast<u32x4_t*>(dst + k * BS) = u32x4_t{w[0], w[1], w[2], w[3]};
-                    else if constexpr (TPL == 8) *reinterpret_cast<uint2*>(dst + k * BS) = make_uint2(w[0], w[1]);
-                    else if constexpr (TPL == 4) *reinterpret_cast<uint32_t*>(dst + k * BS) = w[0];
-                    else *reinterpret_cast<uint16_t*>(dst + k * BS) = (uint16_t)w[0];
-                }
-            } else if (some) {
+                for (int i = 0; i < TPL; ++i) w |= ((y[i][k >> 2] >> (8 * (k & 3))) & 255u) << (8 * i);
+                if constexpr (TPL == 4) *reinterpret_cast<uint32_t*>(dst + k * BS) = w;
+                else if constexpr (TPL == 2) *reinterpret_cast<uint16_t*>(dst + k * BS) = (uint16_t)w;
+                else dst[k * BS] = (uint8_t)w;
+            }
+        } else if (p0 < off + m && p0 + TPL > (grow ? 0 : off)) {
 #pragma unroll
-                for (int i = 0; i < TPL; ++i) {
-                    const int p = p0 + i;
-                    if (p >= off && p < off + m) {
+            for (int i = 0; i < TPL; ++i) {
+                const int p = p0 + i;
+                if (p >= off && p < off + m) {
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) dst[k * BS + i] = (uint8_t)(y[i][k >> 2] >> (8 * (k & 3)));
-                    } else if (grow && p < off) {
+                    for (int k = 0; k < 8; ++k) dst[k * BS + i] = (uint8_t)(y[i][k >> 2] >> (8 * (k & 3)));
+                } else if (grow && p < off) {
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) dst[k * BS + i] = (uint8_t)recode4(dst[k * BS + i]);
-                    }
+                    for (int k = 0; k < 8; ++k) dst[k * BS + i] = (uint8_t)recode4(dst[k * BS + i]);
                 }
             }
-        }
-        // the block's next run, if the rows that follow have one; it reads what this one wrote
-        const unsigned long long more = __ballot(here(slot_at(t + m + lane)));
-        if (!more) break;
-        t += m + __builtin_ctzll(more);
-        s = slots[t];
-        __threadfence_block();
         }
     }
 }
 
+// ROWS == 1: a wave per row.  ROWS == 64: a work-group per 64 rows; where fewer than four blocks begin in them, as in a prompt, it
+// works each run as a whole, else every wave takes every fourth block.  What a run needs to know comes from the slots alone.
+template <int HD, int BS, int ROWS>
+__global__ __launch_bounds__(256) void kv8_append_kernel(const bf16_t* __restrict__ qkv, const int* __restrict__ slots, int T, int Hq, Kv8Cache c) {
+    __shared__ int tops[4];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int ld = (Hq + 2 * c.Hkv) * HD, limit = c.blocks * BS;
+    const int isv = blockIdx.y & 1, h = blockIdx.y >> 1;
+    const int begin = ROWS == 1 ? (int)blockIdx.x * 4 + wave : (int)blockIdx.x * 64;         // T <= 2^30
+    if (begin >= T) return;
+    auto slot_at = [&](int row) { return row >= 0 && row < T ? slots[row] : -1; };
+    // the rows begin - 64 .. begin - 1, begin .. begin + 63 and begin + 64 .. begin + 127
+    const int before = slot_at(begin - 64 + lane), from = slot_at(begin + lane), after = slot_at(begin + 64 + lane);
+    const int last_before = __builtin_amdgcn_readlane(before, 63), left = __shfl_up(from, 1, 64), prev = lane ? left : last_before;
+    // the slots of row and the 63 behind it, `at` its place behind `begin`; out of the registers where they hold them all
+    auto ahead = [&](int at, int row) {
+        const int a = __shfl(from, (at + lane) & 63, 64), b = __shfl(after, (at + lane) & 63, 64);
+        return at > 64 ? slot_at(row + lane) : at + lane < 64 ? a : b;
+    };
+    // rows that begin a run, and of those the ones whose block does not occur in the 64 rows in front of them
+    unsigned long long first = __ballot(lane < ROWS && from >= 0 && from < limit && (prev != from - 1 || from % BS == 0));
+    for (unsigned long long todo = first; todo; todo &= todo - 1) {
+        const int i = __builtin_ctzll(todo), block = __builtin_amdgcn_readlane(from, i) / BS;
+        const int in_front = lane >= i ? before : from;
+        if (__any(in_front >= 0 && in_front / BS == block)) first &= ~(1ull << i);
+    }
+    const bool together = ROWS > 1 && __popcll(first) < 4;
+    for (int turn = 0; first; first &= first - 1, ++turn) {
+        if (ROWS > 1 && !together && (turn & 3) != wave) continue;
+        int at = __builtin_ctzll(first), t = begin + at, s = __builtin_amdgcn_readlane(from, at);
+        const int block = s / BS;
+        for (;;) {
+            const int off = s % BS;
+            // the row's slots follow one another up to the end of the block
+            const int slot = ahead(at, t);                                           // by all lanes: it shuffles
+            const bool in = lane == 0 || (lane < BS - off && slot == s + lane);      // m >= 1: the loop moves on
+            const unsigned long long miss = ~__ballot(in);
+            const int m = miss ? __builtin_ctzll(miss) : 64;
+            if (together) store_run<HD, BS, 256>(qkv, ld, Hq, c, h, isv, t, m, block, off, tops);
+            else store_run<HD, BS, 64>(qkv, ld, Hq, c, h, isv, t, m, block, off, nullptr);
+            // the block's next run, if the 64 rows that follow have one; it reads what this one wrote
+            at += m;
+            const int next = ahead(at, t + m);
+            const unsigned long long more = __ballot(next >= 0 && next / BS == block);
+            if (!more) break;
+            const int gap = __builtin_ctzll(more);
+            t += m + gap;
+            at += gap;
+            s = slots[t];
+            __threadfence_block();
+            if (together) __syncthreads();
+        }
+    }
+}
+
+template <int HD, int BS>
+hipError_t launch_append_bs(hipStream_t st, const bf16_t* qkv, const int* slots, int T, int Hq, const Kv8Cache& c) {
+    // A wave per row while few rows are left over for a wave, or the rows are too few for work-groups of 64 to fill the chip.
+    const bool wave_per_row = (long)T * c.Hkv * 2 <= 16384;
+    if (wave_per_row) kv8_append_kernel<HD, BS, 1><<<dim3((unsigned)((T + 3) / 4), c.Hkv * 2), 256, 0, st>>>(qkv, slots, T, Hq, c);
+    else kv8_append_kernel<HD, BS, 64><<<dim3((unsigned)((T + 63) / 64), c.Hkv * 2), 256, 0, st>>>(qkv, slots, T, Hq, c);
+    return hipGetLastError();
+}
+
 template <int HD>
 hipError_t launch_append(hipStream_t st, const bf16_t* qkv, const int* slots, int T, int Hq, const Kv8Cache& c) {
-    // Rows looked at per wave: one while the chip holds a wave per row, else as many as leave it 4096 waves.
-    const int range = (int)std::min(std::max((long)T * c.Hkv * 2 / 4096, 1L), (long)c.block_size);
-    const dim3 grid((unsigned)(((long)T + 4 * range - 1) / (4 * range)), c.Hkv * 2);
     switch (c.block_size) {
-        case 16: kv8_append_kernel<HD, 16><<<grid, 256, 0, st>>>(qkv, slots, T, range, Hq, c); break;
-        case 32: kv8_append_kernel<HD, 32><<<grid, 256, 0, st>>>(qkv, slots, T, range, Hq, c); break;
-        case 64: kv8_append_kernel<HD, 64><<<grid, 256, 0, st>>>(qkv, slots, T, range, Hq, c); break;
+        case 16: return launch_append_bs<HD, 16>(st, qkv, slots, T, Hq, c);
+        case 32: return launch_append_bs<HD, 32>(st, qkv, slots, T, Hq, c);
+        case 64: return launch_append_bs<HD, 64>(st, qkv, slots, T, Hq, c);
         default: return hipErrorInvalidValue;
     }
-    return hipGetLastError();
 }
 
 // ------------------------------------------------------------------------------------------- attention
