@@ -59,7 +59,7 @@ template <int HD, int ROWS>
 struct TileLoad {
     typedef TokTile<HD> T;
     static constexpr int BYTES = ROWS * T::ROWB, NINST = BYTES / 1024, NI = (NINST + BWD_WAVES - 1) / BWD_WAVES;
-    static_assert(BYTES % 1024 == 0, "whole load instructions");
+    static_assert(BYTES % 1024 == 0 && NINST % NI == 0, "whole load instructions; a wave has NI of them or none, which the waits count on");
     int row[NI], col[NI];
     __device__ void init(int wave, int lane) {
 #pragma unroll
