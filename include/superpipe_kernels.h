@@ -158,7 +158,8 @@ int spk_colsum_bf16(void* stream, const uint16_t* src, int ld, int T, int n, flo
  * the reasons, summed: 1 more rows than max_tokens, 2 more blocks than n_free, 4 a request past max_blocks, 8 a negative
  * length (info[0..2] count all the same, negative lengths as 0).
  * block_size 16, 32 or 64; max_blocks * block_size <= 2^30; 1 <= max_tokens <= 2^30; free_blocks may be NULL with n_free == 0;
- * kv_len must not be cached (hand the two arrays over in turn). */
+ * What the call writes may overlap neither what it reads nor each other (hand cached and kv_len over in turn); an entry of table or
+ * free_blocks that is no block number (negative, or too large for a slot) gives slots of -1. */
 int spk_batch_plan(void* stream, const int32_t* lens, const int32_t* cached, const int32_t* free_blocks, int n_free,
                    int32_t* table, int max_blocks, int32_t* cu, int32_t* kv_len, int32_t* slots, int max_tokens,
                    int32_t* info, int n, int block_size);

@@ -118,7 +118,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void batch_plan_kernel(BatchPlanArgs 
             const int r = owner(s_tok, t), c = g.cached ? g.cached[r] : 0;
             const int pos = c + t - s_tok[r], held = (c + bs - 1) >> lbs, b = pos >> lbs;
             const int block = b < held ? g.table[(size_t)r * g.max_blocks + b] : g.free_blocks[s_new[r] + b - held];
-            slot = block * bs + (pos & (bs - 1));
+            if ((unsigned)block < 1u << (31 - lbs)) slot = block * bs + (pos & (bs - 1));
         }
         g.slots[t] = slot;
     }

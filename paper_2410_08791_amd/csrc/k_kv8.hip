@@ -482,6 +482,7 @@ Kv8Plan plan_kv8(int B, int max_blocks, int block_size, int Hq, int Hkv) {
     const long groups = (long)B * Hkv * ((grp + 15) / 16);
     Kv8Plan p;
     p.per = groups >= 512 && most <= 1024 ? 1024 : groups * most >= 1536L * 768 ? 768 : groups * most >= 512L * 512 ? 512 : 256;
+    p.per = std::max(p.per, (int)((most + 65534) / 65535 + 63) / 64 * 64);      // at most 65535 pieces: a dimension of the grid
     p.splits = (int)((most + p.per - 1) / p.per);
     return p;
 }

@@ -27,16 +27,35 @@ static bool any_null(std::initializer_list<const void*> ptrs) {
 
 constexpr int kMostPositions = 1 << 30;      // of a request, and rows of a packed batch: sums of a few of them fit an int
 
+// An array of 32-bit words; NULL meets nothing.
+struct Ints {
+    const int32_t* p;
+    size_t n;
+    bool meets(const Ints& o) const {
+        const uintptr_t a = (uintptr_t)p, b = (uintptr_t)o.p;
+        return p && o.p && a < b + o.n * 4 && b < a + n * 4;
+    }
+};
+
 static bool block_size_ok(int bs) { return bs == 16 || bs == 32 || bs == 64; }
 
 extern "C" int spk_batch_plan(void* stream, const int32_t* lens, const int32_t* cached, const int32_t* free_blocks, int n_free,
                               int32_t* table, int max_blocks, int32_t* cu, int32_t* kv_len, int32_t* slots, int max_tokens,
                               int32_t* info, int n, int block_size) {
     if (any_null({lens, table, cu, kv_len, slots, info}) || (!free_blocks && n_free > 0)) return SP_ERR_INVALID_ARG;
-    if (misaligned(4, {lens, cached, free_blocks, table, cu, kv_len, slots, info}) || kv_len == cached) return SP_ERR_INVALID_ARG;
+    if (misaligned(4, {lens, cached, free_blocks, table, cu, kv_len, slots, info})) return SP_ERR_INVALID_ARG;
     if (n < 1 || n > kPackedMaxSeqs || n_free < 0 || max_tokens < 1 || max_tokens > kMostPositions || !block_size_ok(block_size) ||
         max_blocks < 1 || max_blocks > kMostPositions / block_size)
         return SP_ERR_INVALID_ARG;
+    // Every work-group reads all lengths, whenever it comes to run: nothing that is written may lie over them, or over one another.
+    const Ints written[] = {{table, (size_t)n * max_blocks}, {cu, (size_t)n + 1}, {kv_len, (size_t)n}, {slots, (size_t)max_tokens}, {info, 4}};
+    const Ints read[] = {{lens, (size_t)n}, {cached, (size_t)n}, {free_blocks, (size_t)n_free}};
+    for (int i = 0; i < 5; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (written[i].meets(written[j])) return SP_ERR_INVALID_ARG;
+        for (const Ints& r : read)
+            if (written[i].meets(r)) return SP_ERR_INVALID_ARG;
+    }
     return st(spk_launch_batch_plan((hipStream_t)stream, BatchPlanArgs{lens, cached, free_blocks, n_free, table, max_blocks, cu, kv_len, slots,
                                                                       max_tokens, info, n, block_size}));
 }

@@ -91,6 +91,15 @@ def test_plan_without_cached_positions_or_free_blocks():
     same_plan(plan([0, 0], [2, 30], [], table, 1, 16), P.batch_plan([0, 0], [2, 30], [], table, 1, 16))
 
 
+def test_plan_of_entries_that_are_no_blocks():
+    """Rows that would go to them have no slot."""
+    table = np.array([[2 ** 28 + 1, 9], [-3, 9], [2 ** 31 - 1, 9], [2 ** 27 - 1, 9]], np.int32)
+    got = plan([2, 2, 20, 2], [3, 3, 3, 3], [2 ** 27, 0], table, 26, 16)
+    slots = np.full(26, -1)
+    slots[24:] = (2 ** 27 - 1) * 16 + np.array([3, 4])
+    assert np.array_equal(got[2], slots) and list(got[4]) == [26, 1, 20, 0] and got[3][2, 1] == 2 ** 27
+
+
 @pytest.mark.parametrize("lens,cached,n_free,max_tokens,why", [
     ([5, 20], [0, 0], 3, 24, 1), ([5, 20], [0, 0], 2, 25, 2), ([5, 20], [0, 40], 9, 25, 4), ([5, -1], [0, 0], 9, 25, 8), ([5, 1], [-2, 0], 9, 25, 8),
     ([2 ** 31 - 1, 2 ** 31 - 1], [0, 0], 2, 9, 7), ([5, 20], [2 ** 31 - 1, 0], 9, 25, 4),
@@ -158,6 +167,16 @@ def test_packed_attention(lens, spare, hq, hkv, hd, causal):
 ])
 def test_packed_attention_large(lens, hq, hkv, hd, causal):
     check_forward(lens, 3, hq, hkv, hd, causal)
+
+
+@pytest.mark.parametrize("lens,spare,hq,hkv,hd", [
+    ([127, 128, 129, 1, 300, 0, 31], 3, 24, 6, 64), ([33, 257, 576, 0, 64], 0, 12, 4, 80), ([1030, 77, 1], 5, 18, 2, 128), ([1, 2, 3], 0, 200, 1, 128),
+    ([3] * 70 + [200] + [0] * 3 + [9] * 60, 4, 8, 8, 64),
+])
+@pytest.mark.parametrize("causal", [1, 0])
+def test_packed_attention_of_many_heads(lens, spare, hq, hkv, hd, causal):
+    """Blocks of 128 queries, which small batches do not take."""
+    check_forward(lens, spare, hq, hkv, hd, causal)
 
 
 def test_packed_attention_of_many_requests():
@@ -244,6 +263,41 @@ def check_backward(lens, spare, hq, hkv, hd, causal, seed=0):
 @pytest.mark.parametrize("causal", [1, 0])
 def test_packed_attention_backward(lens, spare, hq, hkv, hd, causal):
     check_backward(lens, spare, hq, hkv, hd, causal)
+
+
+@pytest.mark.parametrize("lens,spare,hq,hkv,hd", [
+    ([127, 128, 129, 1, 300], 3, 32, 16, 64), ([1, 31, 32, 33, 64, 65, 127, 128, 129, 130] * 2, 1, 32, 32, 64),
+    ([3] * 70 + [200] + [0] * 3 + [9] * 60, 4, 5, 5, 64), ([33, 257, 96], 0, 40, 20, 80), ([33, 257, 0, 130], 2, 20, 20, 80),
+    ([500, 0, 12, 129], 9, 48, 24, 128),
+])
+@pytest.mark.parametrize("causal", [1, 0])
+def test_packed_attention_backward_of_many_heads(lens, spare, hq, hkv, hd, causal):
+    """Work-groups of more keys, which small batches do not take."""
+    check_backward(lens, spare, hq, hkv, hd, causal)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_packed_attention_behind_four_gigabytes(hd):
+    """Rows, outputs and gradients whose offsets in bytes pass 32 bits: the last request of a long buffer, the rows in front of
+    it belonging to nobody."""
+    hq, hkv, n, far = 24, 24, 150, 2 ** 32 // (72 * hd * 2) + 3
+    rng, T = np.random.default_rng(hd), far + n
+    bits, vals = rand_bf16(rng, (n, 72 * hd))
+    db, dv = rand_bf16(rng, (n, hq * hd), 0.5)
+    qkv, do, o, dx = (torch.zeros((T, w * hd), dtype=torch.int16, device=DEV) for w in (72, hq, hq, 72))
+    qkv[far:], do[far:] = dev_u16(bits), dev_u16(db)
+    lse, cu = torch.zeros((hq, T), device=DEV), i32([far, T])
+    scratch = torch.zeros(sp.spk_attention_packed_bwd_scratch_bytes(T, hq), dtype=torch.uint8, device=DEV)
+    assert sp.spk_attention_packed(stream_ptr(), ptr(qkv), ptr(cu), ptr(o), ptr(lse), 1, T, hq, hkv, hd, 1) == sp.SP_OK
+    assert sp.spk_attention_packed_bwd(stream_ptr(), ptr(qkv), ptr(cu), ptr(o), ptr(do), ptr(lse), ptr(scratch), ptr(dx), 1, T, hq, hkv,
+                                       hd, 1) == sp.SP_OK
+    torch.cuda.synchronize()
+    assert not bool(o[:far].any()) and not bool(dx[:far].any())
+    got, got_dx = bf16_vals(host_u16(o[far:])).reshape(n, hq, hd), bf16_vals(host_u16(dx[far:])).reshape(n, -1, hd)
+    want, _, weight = P.attention_packed(vals, [0, n], hq, hkv, hd, True)
+    assert np.all(np.abs(got - want) <= STEP * (weight + np.abs(want)) + FP32 * weight)
+    want, rounded, entering = P.attention_packed_bwd(vals, [0, n], got, dv, lse[:, far:].cpu().numpy().astype(np.float64), hq, hkv, hd, True)
+    assert np.all(np.abs(got_dx - want) <= STEP * (rounded + np.abs(want)) + FP32 * entering)
 
 
 def test_packed_attention_backward_large():
@@ -350,6 +404,28 @@ def test_append_runs_of_one_block_are_stored_in_order():
         check_append(rng, bits, bf16_vals(bits), slots, 16, hkv, hkv, 64, 4)
 
 
+@pytest.mark.parametrize("hd,bs", [(64, 16), (128, 64), (128, 32)])
+def test_append_single_tokens_of_many_requests(hd, bs):
+    """A row per request at any place of its block, with so many heads that work-groups take 64 rows; blocks in no order."""
+    rng = np.random.default_rng(hd + bs)
+    T, hkv, blocks = 230, 40, 260
+    slots = (rng.permutation(blocks)[:T] * bs + rng.integers(0, bs, T)).astype(np.int32)
+    slots[::50] = -1
+    bits, _ = rand_bf16(rng, (T, 3 * hkv * hd))
+    check_append(rng, bits, bf16_vals(bits), slots, bs, hkv, hkv, hd, blocks)
+
+
+def test_append_runs_of_one_block_with_many_heads():
+    """The runs above by work-groups of 64 rows: few blocks (all waves work a run together) and many (each wave its own)."""
+    rng = np.random.default_rng(16)
+    runs = np.array([3, 4, 4, 5, 20, -1, 6, 2, 3, 21, 22, 9, 40, 41, 9, 9] + [-1] * 40 + [23, 42, 10, 43] + [-1] * 62 + [11, 44])
+    many = np.concatenate([runs, 48 + np.arange(16), [70, 80, 96, 112, 71, 81, 97, 113, 72, 82], [60] * 3, 128 + np.arange(48), [83]])
+    few = np.concatenate([[3, 4, 4, 5], [-1] * 30, [6, 7, 7, 2, 3], [-1] * 62, [4, 5], 16 + np.arange(16), [-1] * 50, 30 + np.arange(20)])
+    for slots in (many, few):
+        bits, _ = rand_bf16(rng, (len(slots), 3 * 64 * 64))
+        check_append(rng, bits, bf16_vals(bits), slots.astype(np.int32), 16, 64, 64, 64, 14)
+
+
 def test_append_edge_values():
     """Zeros, the smallest and largest bf16 values, ties between codes, infinities and NaN."""
     rng = np.random.default_rng(2)
@@ -435,10 +511,47 @@ def test_cache_attention(bs, hq, hkv, hd):
 @pytest.mark.parametrize("lens,bs,hq,hkv,hd,extra", [
     ([5000, 3], 16, 8, 2, 128, 0), ([700, 4099, 0, 1], 64, 4, 4, 64, 90), ([20000], 32, 2, 1, 128, 0), ([300] * 40, 16, 8, 8, 64, 40),
     ([1, 1025, 511, 512, 513], 32, 64, 8, 128, 7),
+    ([900, 1, 64] * 24, 16, 8, 8, 64, 7),                        # heads and requests enough: no pieces
+    ([767, 768, 769, 1] * 10, 64, 16, 8, 128, 60),
 ])
 def test_cache_attention_in_pieces(lens, bs, hq, hkv, hd, extra):
     """Positions shared out over work-groups; pieces that nobody fills."""
     check_cache_attention(lens, bs, hq, hkv, hd, extra)
+
+
+def test_cache_behind_four_gigabytes():
+    """Blocks whose offsets in bytes pass 32 bits, in both halves of the cache."""
+    hq, hkv, hd, bs = 8, 8, 128, 64
+    block = hkv * bs * hd
+    blocks = 2 ** 32 // block + 5
+    k8, v8 = (torch.zeros(blocks * block, dtype=torch.uint8, device=DEV) for _ in range(2))
+    scales = torch.zeros(blocks * hkv * 2, device=DEV)
+    table = np.array([[blocks - 1, 3], [blocks - 3, blocks - 2]])
+    lens = np.array([70, 128])
+    _, _, slots, _, _ = P.batch_plan(lens, [0, 0], table.reshape(-1), np.zeros((2, 2)), 198, bs)
+    rng = np.random.default_rng(5)
+    bits, vals = rand_bf16(rng, (198, (hq + 2 * hkv) * hd))
+    q, s = dev_u16(bits), i32(slots)
+    assert sp.spk_kv8_append(stream_ptr(), ptr(q), ptr(s), ptr(k8), ptr(v8), ptr(scales), 198, blocks, bs, hq, hkv, hd) == sp.SP_OK
+    torch.cuda.synchronize()
+    used = [int(b) for b in table.reshape(-1)]
+    near = {b: i for i, b in enumerate(used)}
+    z = np.zeros((4, hkv, bs, hd), np.uint8), np.zeros((4, hkv, hd, bs), np.uint8), np.zeros((4, hkv, 2))
+    want = P.kv8_append(vals, np.array([near[v // bs] * bs + v % bs for v in map(int, slots)]), *z, bs, hq, hkv, hd)
+    for pool, w in zip((k8, v8, scales), want):
+        for b, i in near.items():
+            assert np.array_equal(pool.reshape(blocks, -1)[b].cpu().numpy(), w[i].reshape(-1)), b
+        assert not bool(pool.reshape(blocks, -1)[4:blocks - 4].any())
+    qbits, qv = rand_bf16(rng, (2, (hq + 2 * hkv) * hd), 0.3)
+    o = torch.zeros((2, hq * hd), dtype=torch.int16, device=DEV)
+    x, t, n = dev_u16(qbits), i32(table), i32(lens)
+    assert sp.spk_kv8_attention_scratch_bytes(2, 2, bs, hq, hkv, hd) == 0
+    assert sp.spk_kv8_attention(stream_ptr(), ptr(x), ptr(k8), ptr(v8), ptr(scales), ptr(t), ptr(n), ptr(o), None, 2, blocks, bs, 2, hq, hkv,
+                                hd) == sp.SP_OK
+    torch.cuda.synchronize()
+    ref, weight = P.kv8_attention(qv[:, :hq * hd].reshape(2, hq, hd), *want, np.array([[0, 1], [2, 3]]), lens, bs)
+    got = bf16_vals(host_u16(o)).reshape(2, hq, hd)
+    assert np.all(np.abs(got - ref) <= STEP * (weight + np.abs(ref)) + FP32 * weight)
 
 
 def test_cache_attention_without_positions_and_bad_entries():

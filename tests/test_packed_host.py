@@ -54,7 +54,8 @@ def test_oracle_gradient_against_differences(causal):
 
 def test_plan_refusals():
     p = 4096         # an aligned address that is never followed: every call below ends in the argument checks
-    good = dict(lens=p, cached=p + 64, free=p, n_free=4, table=p, max_blocks=4, cu=p, kv_len=p, slots=p, max_tokens=8, info=p, n=3, bs=16)
+    good = dict(lens=p, cached=p + 64, free=p + 128, n_free=4, table=p + 192, max_blocks=4, cu=p + 256, kv_len=p + 320, slots=p + 384,
+                max_tokens=8, info=p + 448, n=3, bs=16)
 
     def call(**kw):
         a = dict(good, **kw)
@@ -63,7 +64,8 @@ def test_plan_refusals():
     for kw in (dict(lens=None), dict(table=None), dict(cu=None), dict(kv_len=None), dict(slots=None), dict(info=None), dict(free=None),
                dict(n=0), dict(n=4097), dict(n_free=-1), dict(max_tokens=0), dict(max_tokens=(1 << 30) + 1), dict(bs=8), dict(bs=48),
                dict(bs=128), dict(max_blocks=0), dict(max_blocks=(1 << 26) + 1), dict(lens=p + 2), dict(slots=p + 1),
-               dict(cached=p, kv_len=p)):
+               dict(kv_len=p), dict(kv_len=p + 64), dict(cached=p + 260), dict(cu=p - 12), dict(table=p + 140), dict(slots=p + 100),
+               dict(slots=p + 324), dict(info=p + 412), dict(info=p + 264), dict(max_tokens=17)):
         assert call(**kw) == BAD, kw
 
 
@@ -81,7 +83,7 @@ def test_attention_refusals():
         return sp.spk_attention_packed_bwd(None, a["qkv"], a["cu"], a["o"], a["dO"], a["lse"], a["scratch"], a["dqkv"], a["n"], a["T"],
                                            a["hq"], a["hkv"], a["hd"], 1)
     wrong = [dict(qkv=None), dict(cu=None), dict(o=None), dict(n=0), dict(n=4097), dict(T=0), dict(T=(1 << 30) + 1), dict(hq=3),
-             dict(hq=0), dict(hkv=0), dict(hd=96), dict(hd=256), dict(qkv=p + 2), dict(o=p + 8), dict(cu=p + 2), dict(T=1 << 29, hq=64)]
+             dict(hq=0), dict(hkv=0), dict(hq=16386), dict(hd=96), dict(hd=256), dict(qkv=p + 2), dict(o=p + 8), dict(cu=p + 2), dict(T=1 << 29, hq=64)]
     for kw in wrong:
         assert call(**kw) == BAD and call_bwd(**kw) == BAD, kw
     for kw in (dict(dO=None), dict(lse=None), dict(scratch=None), dict(dqkv=None), dict(dqkv=p + 4), dict(scratch=p + 4)):
@@ -126,7 +128,7 @@ def test_kv8_plan_covers_the_table():
         mb = int(2.0 ** rng.uniform(0, 26 - np.log2(bs / 16)))
         assert sp.spk_kv8_plan(B, mb, bs, hkv * g, hkv, out) == sp.SP_OK
         splits, per = out
-        assert splits >= 1 and per % 64 == 0 and splits * per >= mb * bs and (splits - 1) * per < mb * bs
+        assert 1 <= splits <= 65535 and per % 64 == 0 and splits * per >= mb * bs and (splits - 1) * per < mb * bs
         need = sp.spk_kv8_attention_scratch_bytes(B, mb, bs, hkv * g, hkv, 128)
         assert need == (0 if splits == 1 else B * hkv * g * splits * 130 * 4)
         # a row of partial results for every 256 positions is room enough
