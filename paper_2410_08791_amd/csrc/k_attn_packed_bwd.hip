@@ -4,8 +4,10 @@
 //   dq    -- a work-group owns 128 queries of one head and walks the keys.
 // P = exp(s - lse), dS = P (dP - delta), dP = dO V^T; layouts and tiles are those of k_attn_bwd.hip.
 //
-// What bounds it: 7 products of 2 hd flops per pair of a query and a key on the matrix pipe, 1 KB of LDS per MFMA of 32
-// cycles (which four SIMDs drawing at once would all but use up), and the arithmetic of P and dS on the vector pipe.  Every
+// What bounds it: 7 products of 2 hd flops per pair of a query and a key on the matrix pipe, 1 KB of LDS and more per MFMA of
+// 32 cycles, and the arithmetic of P and dS on the vector pipe.  At head_dim 128 the eight waves of a CU take 40 KB each out of
+// LDS for the 32 MFMAs of 32 keys and 32 queries in dk/dv (the keys have no room in registers): 2560 cycles of LDS beside 2048
+// of the matrix pipes, of some 3600 that such a step takes.  Batches of few long sequences wait for their longest chain.  Every
 // wave therefore reads its fragments a few MFMAs ahead, in an order that the source fixes, and works P beside the MFMAs
 // of dP, and dS beside those of dV (dk/dv) or of the next 32 keys' scores (dq).  One launch: a short batch has too few
 // blocks of either kind to fill the chip.  Four waves each, two work-groups per CU: with one of eight, nothing covered
@@ -288,7 +290,10 @@ struct DkvCfg {
     static constexpr int SUBS = BWD_WAVES / KG, ROWS = 32 * SUBS, KEYS = 32 * KG;
     static constexpr bool K_IN_LDS = HD == 128;       // K fragments would not fit beside the accumulators
     static constexpr int TILE = ROWS * T::ROWB, STAGE = 2 * TILE;
-    static constexpr int KBYTES = K_IN_LDS ? KEYS * T::ROWB : 0;
+    // k-steps of the keys that are kept there, 32 keys of a k-step in the order of a wave's lanes; all, or all but one where
+    // two work-groups fit a CU only so: that one is read again for every tile
+    static constexpr int KSTEP = KEYS * 32, KIN = !K_IN_LDS ? 0 : 2 * STAGE + T::NKS * KSTEP + 4 * ROWS * 4 <= 80 * 1024 ? T::NKS : T::NKS - 1;
+    static constexpr int KBYTES = KIN * KSTEP;
     static constexpr int bytes(int stages) { return stages * STAGE + KBYTES + stages * 2 * ROWS * 4; }
     static constexpr int STG = HD == 128 || bytes(3) > 80 * 1024 ? 2 : 3;
     static constexpr int LDS = std::max(bytes(STG), SUBS > 1 ? (SUBS - 1) * KG * T::NMT * 16 * 256 : 0);
@@ -342,19 +347,31 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
         if (f_q >= len) { f_q = q_begin; ++f_head; }
     };
     if (C::K_IN_LDS) {
-        TileLoad<HD, C::KEYS> kl;
-        kl.init(wave, lane);
-        kl.issue(sKeys, wave, kbase + (size_t)k0 * ld, ld, len - k0);
-    }
-    bf16x8_t kf_reg[C::K_IN_LDS ? 1 : NK], vf[NK];
-    {
-        const size_t kr = min(kj, len - 1);
+#if defined(__HIP_DEVICE_COMPILE__)
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(kbase + (size_t)k0 * ld), 0, min(len - k0, C::KEYS) * ld * 2, 0x00020000);
 #pragma unroll
-        for (int ks = 0; ks < NK; ++ks) {
-            if (!C::K_IN_LDS) kf_reg[C::K_IN_LDS ? 0 : ks] = *reinterpret_cast<const bf16x8_t*>(kbase + kr * ld + half * 8 + ks * 16);
-            vf[ks] = *reinterpret_cast<const bf16x8_t*>(vbase + kr * ld + half * 8 + ks * 16);
+        for (int i = 0; i < (C::KIN * KG + BWD_WAVES - 1) / BWD_WAVES; ++i) {
+            const int j = wave + i * BWD_WAVES;
+            if (j < C::KIN * KG)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void_ptr)(sKeys + j * 1024), 16, (j % KG * 32 + l32) * ld * 2 + half * 16,
+                                                         j / KG * 32, 0, 0);
         }
+#endif
     }
+    bf16x8_t kf_reg[NK], vf[NK];                      // kf_reg: of the k-steps that are not in LDS
+    const size_t krow = (size_t)min(kj, len - 1) * ld + half * 8;
+#pragma unroll
+    for (int ks = 0; ks < NK; ++ks) {
+        if (!C::K_IN_LDS) kf_reg[ks] = *reinterpret_cast<const bf16x8_t*>(kbase + krow + ks * 16);
+        vf[ks] = *reinterpret_cast<const bf16x8_t*>(vbase + krow + ks * 16);
+    }
+    // The k-step that is neither in LDS nor, but between two tiles, in registers: its load lands with the next tile's.
+    auto k_again = [&]() __attribute__((always_inline)) {
+        size_t row = krow;
+        asm volatile("" : "+v"(row));                 // not the load before
+        kf_reg[NK - 1] = *reinterpret_cast<const bf16x8_t*>(kbase + row + (NK - 1) * 16);
+    };
+    if constexpr (C::K_IN_LDS && C::KIN < NK) k_again();
     FragAt<HD> at;
     at.init(lane);
     f32x16_t dk[T::NMT], dv[T::NMT];
@@ -381,7 +398,7 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
             float4 l4[4], d4[4];
             auto read_s = [&](int i) __attribute__((always_inline)) {
                 qf[i] = at.row(smem, q_at, i, 0);
-                if (C::K_IN_LDS) kf[i] = at.row(sKeys, kg * 32 * T::ROWB, i, 0);
+                kf[i] = i < C::KIN ? lds_b128(sKeys + i * C::KSTEP + kg * 1024 + lane * 16) : kf_reg[i];
             };
             auto read_p = [&](int i) __attribute__((always_inline)) { df[i] = at.row(smem, q_at, i, C::TILE); };
             auto read_v = [&](int i) __attribute__((always_inline)) { tv[i] = at.tr(smem, q_at, i % T::NMT, C::TILE + 16 * (i / T::NMT) * T::ROWB); };
@@ -396,7 +413,7 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
                 if (i + PF < NK) read_s(i + PF);
                 else read_p(i + PF - NK);
                 if (i + 1 == NK) l4[0] = lds_f4(lrow);
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[i], C::K_IN_LDS ? kf[i] : kf_reg[C::K_IN_LDS ? 0 : i], i ? s : zeros(), 0, 0, 0);
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[i], kf[i], i ? s : zeros(), 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
             if ((g.causal && qs < wk0 + 31) || qs + 32 > len) {
@@ -408,6 +425,7 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
                     s[e] = q >= first && q < end ? s[e] : -INFINITY;
                 }
             }
+            if constexpr (C::K_IN_LDS && C::KIN < NK) k_again();
             // dP beside P, which takes the place of the scores; row values a step ahead of their use: registers are short here
 #pragma unroll
             for (int i = 0; i < NK; ++i) {
@@ -520,17 +538,18 @@ hipError_t launch_bwd(hipStream_t st, const AttnBwdArgs& b, const PackedShape& a
 
 // Keys of a dk/dv work-group.  Its chain is the queries of all heads that share them, 32 at a time: with 128 keys per group that
 // is what a batch of few groups waits for, with fewer the waves share out the queries and the chain is a half or a quarter.
-// But each group loads all queries, and at head_dim 128 only one of it fits a CU then.  us for 128, 64, 32 keys (groups of 128
-// keys in brackets):
+// But each group loads all queries.  us for 128, 64, 32 keys (groups of 128 keys in brackets):
 //   head_dim 64:  900 + 200 tokens, 8/4 heads (40) 53.5 30.3 21.4;  3 x 2000, 8/2 (98) 211 115 85;  3000, 8/8 (192) 84 58 69;
 //                 8 x 512, 16/16 (640) 45.3 44.7 55.3;  12 x 300, 32/32 (1280) 58.7 61.2 81.0
 //   head_dim 80:  1500 + 300, 8/2 (32) 161 91 58;  6 x 700, 32/8 (304) 125 97 149;  8 x 577, 16/16 (704) 60.9 63.9 112.6; 4 x 1000,
 //                 8/8 (280), where the chain is one head, 42.5 45.1 61.7
-//   head_dim 128: 3 x 2000, 8/2 (98) 274 155 165;  3000, 8/8 (192) 118 108 132;  6 x 700, 32/8 (304) 158 161 201
+//   head_dim 128: 3 x 2000, 8/2 (98) 274 174;  3000, 8/8 (192) 118 93;  4000, 32/8 (256) 615 444;  6 x 700, 32/8 (304) 134 125;
+//                 20 x 200, 32/8 (408) 80 86;  4 x 2048, 64/8 (544) 971 1010;  3000, 12/12 (288) 145 141; 1541 + 1026 + 400, 16/16
+//                 (416) 78 90
 template <int HD>
 hipError_t launch_hd(hipStream_t st, const AttnBwdArgs& b, const PackedShape& a) {
     const long groups = ((long)a.T / 128 + a.n) * a.Hkv;
-    if (HD == 128) return groups <= 192 ? launch_bwd<HD, 2>(st, b, a) : launch_bwd<HD, 4>(st, b, a);
+    if (HD == 128) return groups <= (a.Hq > a.Hkv ? 400 : 288) ? launch_bwd<HD, 2>(st, b, a) : launch_bwd<HD, 4>(st, b, a);
     if constexpr (HD != 128)
         if (groups <= (HD == 64 ? 128 : 64)) return launch_bwd<HD, 1>(st, b, a);
     if (HD == 64 ? groups <= 640 : groups <= 512 && a.Hq > a.Hkv) return launch_bwd<HD, 2>(st, b, a);

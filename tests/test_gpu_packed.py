@@ -268,7 +268,7 @@ def test_packed_attention_backward(lens, spare, hq, hkv, hd, causal):
 @pytest.mark.parametrize("lens,spare,hq,hkv,hd", [
     ([127, 128, 129, 1, 300], 3, 32, 16, 64), ([1, 31, 32, 33, 64, 65, 127, 128, 129, 130] * 2, 1, 32, 32, 64),
     ([3] * 70 + [200] + [0] * 3 + [9] * 60, 4, 5, 5, 64), ([33, 257, 96], 0, 40, 20, 80), ([33, 257, 0, 130], 2, 20, 20, 80),
-    ([500, 0, 12, 129], 9, 48, 24, 128),
+    ([500, 0, 12, 129], 9, 48, 24, 128), ([257, 0, 12, 129], 2, 60, 60, 128), ([130, 1, 70, 0, 0, 9], 0, 140, 70, 128),
 ])
 @pytest.mark.parametrize("causal", [1, 0])
 def test_packed_attention_backward_of_many_heads(lens, spare, hq, hkv, hd, causal):
