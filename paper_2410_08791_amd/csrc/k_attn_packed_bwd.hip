@@ -1,8 +1,9 @@
 // Backward of the attention over packed prompts: dq, dk, dv from q, k, v, dO, the forward's log-sum-exp and
-// delta = rowsum(dO * O), without atomics, in one launch of two kinds of work-groups that do not depend on one another:
+// delta = rowsum(dO * O), without atomics, in one launch (behind a small one for -delta) of two kinds of work-groups that
+// do not depend on one another:
 //   dk/dv -- a work-group owns 32 KG keys of one key/value head and walks the queries of every query head that shares it;
 //   dq    -- a work-group owns 128 queries of one head and walks the keys.
-// P = exp(s - lse), dS = P (dP - delta), dP = dO V^T; layouts and tiles are those of k_attn_bwd.hip.
+// P = exp(s - lse), dS = P (dP - delta), dP = dO V^T (in dk/dv its sums begin at -delta); layouts and tiles are those of k_attn_bwd.hip.
 //
 // What bounds it: 7 products of 2 hd flops per pair of a query and a key on the matrix pipe, 1 KB of LDS and more per MFMA of
 // 32 cycles, and the arithmetic of P and dS on the vector pipe.  At head_dim 128 the eight waves of a CU take 40 KB each out of
@@ -104,7 +105,7 @@ __device__ __forceinline__ f32x16_t zeros() {
 
 struct BwdDev {
     const bf16_t *qkv, *dO;
-    const float *lse, *delta;
+    const float *lse, *minus_delta;
     bf16_t* dqkv;
     const int* cu;
     int n, T, Hq, Hkv, causal;
@@ -156,7 +157,7 @@ __device__ __forceinline__ void dq_group(const BwdDev& g, unsigned char* smem, i
             dof[ks] = *reinterpret_cast<const bf16x8_t*>(dp + ks * 16);
         }
     }
-    const float lse_q = g.lse[row0 + qr] * LOG2E, delta_q = g.delta[row0 + qr];
+    const float lse_q = g.lse[row0 + qr] * LOG2E, minus_delta = g.minus_delta[row0 + qr];
     issue(0);
     if (STAGES<HD> > 2 && ntiles > 1) issue(1);
     FragAt<HD> at;
@@ -205,7 +206,7 @@ __device__ __forceinline__ void dq_group(const BwdDev& g, unsigned char* smem, i
             }
 #pragma unroll
             for (int e = 8 * i / NK; e < 8 * (i + 1) / NK; ++e) {
-                uint32_t w = pack2(s[2 * e] * (dp[2 * e] - delta_q), s[2 * e + 1] * (dp[2 * e + 1] - delta_q));
+                uint32_t w = pack2(s[2 * e] * (dp[2 * e] + minus_delta), s[2 * e + 1] * (dp[2 * e + 1] + minus_delta));
                 asm volatile("" : "+v"(w));
                 ds[e >> 2][e & 3] = w;
             }
@@ -318,7 +319,7 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
     const bf16_t* kbase = g.qkv + tok0 * ld + (size_t)(Hq + kvh) * HD;
     const bf16_t* vbase = kbase + (size_t)Hkv * HD;
     unsigned char* sKeys = smem + C::STG * C::STAGE;
-    float* rowvals = reinterpret_cast<float*>(smem + C::STG * C::STAGE + C::KBYTES);       // [stage][lse | delta][ROWS]
+    float* rowvals = reinterpret_cast<float*>(smem + C::STG * C::STAGE + C::KBYTES);       // [stage][lse | -delta][ROWS]
 
     // the tiles in walking order: (query head of the group, ROWS queries)
     const int q_begin = g.causal ? k0 / C::ROWS * C::ROWS : 0;
@@ -332,10 +333,10 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
         unsigned char* st = smem + stage * C::STAGE;
         tl.issue(st, wave, g.qkv + (tok0 + f_q) * ld + (size_t)h * HD, ld, len - f_q);
         tl.issue(st + C::TILE, wave, g.dO + (tok0 + f_q) * ld_do + (size_t)h * HD, ld_do, len - f_q);
-        // wave 0 the rows' log-sum-exps, wave 1 their deltas
+        // wave 0 the rows' log-sum-exps, wave 1 their -deltas
 #if defined(__HIP_DEVICE_COMPILE__)
         if (wave < 2 && lane < C::ROWS) {
-            const float* src = (wave ? g.delta : g.lse) + (size_t)h * g.T + tok0 + f_q;
+            const float* src = (wave ? g.minus_delta : g.lse) + (size_t)h * g.T + tok0 + f_q;
             const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(src), 0, min(len - f_q, C::ROWS) * 4, 0x00020000);
 #pragma unroll
             for (int i = 0; i < NR; ++i)
@@ -395,7 +396,7 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
             f32x16_t s, dp;
             u32x4_t pw[2], ds[2];
             bf16x8_t qf[NK], kf[NK], df[NK], tv[NV], tk[NV];
-            float4 l4[4], d4[4];
+            float4 l4[4];
             auto read_s = [&](int i) __attribute__((always_inline)) {
                 qf[i] = at.row(smem, q_at, i, 0);
                 kf[i] = i < C::KIN ? lds_b128(sKeys + i * C::KSTEP + kg * 1024 + lane * 16) : kf_reg[i];
@@ -413,6 +414,14 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
                 if (i + PF < NK) read_s(i + PF);
                 else read_p(i + PF - NK);
                 if (i + 1 == NK) l4[0] = lds_f4(lrow);
+                if (i + 2 >= NK) {                        // dP begins at -delta
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const float4 d = lds_f4(lrow + C::ROWS + ((i + 2 - NK) * 2 + k) * 8);
+                        const int e = ((i + 2 - NK) * 2 + k) * 4;
+                        dp[e] = d.x; dp[e + 1] = d.y; dp[e + 2] = d.z; dp[e + 3] = d.w;
+                    }
+                }
                 s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[i], kf[i], i ? s : zeros(), 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -431,11 +440,10 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
             for (int i = 0; i < NK; ++i) {
                 if (i + PF < NK) read_p(i + PF);
                 else read_v(i + PF - NK);
-                if (i + 1 == NK) d4[0] = lds_f4(lrow + C::ROWS);
 #pragma unroll
                 for (int k = 1; k < 4; ++k)
                     if (step_of(2 * k, NK, 8) == i + 1) l4[k] = lds_f4(lrow + k * 8);
-                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(df[i], vf[i], i ? dp : zeros(), 0, 0, 0);
+                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(df[i], vf[i], dp, 0, 0, 0);
 #pragma unroll
                 for (int e = 8 * i / NK; e < 8 * (i + 1) / NK; ++e) {
                     const float4 l = l4[e >> 1];
@@ -454,14 +462,10 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
             for (int i = 0; i < NV; ++i) {
                 if (i + PF < NV) read_v(i + PF);
                 else read_k(i + PF - NV);
-#pragma unroll
-                for (int k = 1; k < 4; ++k)
-                    if (step_of(2 * k, NV, 8) == i + 1) d4[k] = lds_f4(lrow + C::ROWS + k * 8);
                 dv[i % T::NMT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tv[i], __builtin_bit_cast(bf16x8_t, pw[i / T::NMT]), dv[i % T::NMT], 0, 0, 0);
 #pragma unroll
                 for (int e = 8 * i / NV; e < 8 * (i + 1) / NV; ++e) {
-                    const float4 d = d4[e >> 1];
-                    uint32_t w = pack2(s[2 * e] * (dp[2 * e] - ((e & 1) ? d.z : d.x)), s[2 * e + 1] * (dp[2 * e + 1] - ((e & 1) ? d.w : d.y)));
+                    uint32_t w = pack2(s[2 * e] * dp[2 * e], s[2 * e + 1] * dp[2 * e + 1]);
                     asm volatile("" : "+v"(w));
                     ds[e >> 2][e & 3] = w;
                 }
@@ -515,6 +519,36 @@ __device__ __forceinline__ void dkv_group(const BwdDev& g, unsigned char* smem, 
     take(dv, C::SUBS > 1 ? 1 : 0, Hkv, 1.0f);
 }
 
+// -delta = -rowsum(dO * O), [Hq][T].  HBM-bound: LANES lanes per (token, head), which lie side by side in dO and O, and four such
+// rows on their way per lane.
+template <int HD>
+__global__ __launch_bounds__(256) void minus_delta_kernel(const bf16_t* __restrict__ dO, const bf16_t* __restrict__ o, float* __restrict__ minus_delta,
+                                                          int T, int Hq) {
+    constexpr int LANES = HD == 64 ? 8 : 16, PER = 256 / LANES, BATCH = 4;
+    const int sub = threadIdx.x % LANES, total = T * Hq, first = (int)blockIdx.x * (PER * BATCH) + threadIdx.x / LANES;
+    u32x4_t a[BATCH], b[BATCH];
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+        const size_t at = (size_t)min(first + i * PER, total - 1) * HD + min(sub * 8, HD - 8);
+        a[i] = *reinterpret_cast<const u32x4_t*>(dO + at);
+        b[i] = *reinterpret_cast<const u32x4_t*>(o + at);
+    }
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s = fmaf(bf_hi(a[i][k]), bf_hi(b[i][k]), fmaf(bf_lo(a[i][k]), bf_lo(b[i][k]), s));
+        if (sub * 8 >= HD) s = 0.f;
+#pragma unroll
+        for (int x = LANES / 2; x > 0; x >>= 1) s += __shfl_xor(s, x, 64);
+        const int it = first + i * PER;
+        if (sub == 0 && it < total) {
+            const int tok = it / Hq, h = it - tok * Hq;
+            minus_delta[(size_t)h * T + tok] = -s;
+        }
+    }
+}
+
 template <int HD, int KG>
 __global__ __launch_bounds__(BWD_WAVES * 64, 2) void attn_packed_bwd_kernel(BwdDev g, int dkv_groups) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem_bwd[];
@@ -523,13 +557,13 @@ __global__ __launch_bounds__(BWD_WAVES * 64, 2) void attn_packed_bwd_kernel(BwdD
 }
 
 template <int HD, int KG>
-hipError_t launch_bwd(hipStream_t st, const AttnBwdArgs& b, const PackedShape& a) {
+hipError_t launch_bwd(hipStream_t st, const PackedBwdArgs& b, const PackedShape& a) {
     constexpr int LDS = std::max(DqCfg<HD>::LDS, DkvCfg<HD, KG>::LDS);
     static LdsLimitOnce lim;
     hipError_t e = lim.set(reinterpret_cast<const void*>(attn_packed_bwd_kernel<HD, KG>), LDS);
     if (e != hipSuccess) return e;
     const float scale = 1.0f / sqrtf((float)HD);
-    const BwdDev g{b.qkv, b.dO, b.lse, b.delta, b.dqkv, a.cu, a.n, a.T, a.Hq, a.Hkv, a.causal, scale, scale * LOG2E};
+    const BwdDev g{b.qkv, b.dO, b.lse, b.minus_delta, b.dqkv, a.cu, a.n, a.T, a.Hq, a.Hkv, a.causal, scale, scale * LOG2E};
     const long slots = (long)a.T / 128 + a.n;
     const long kv = (((long)a.T / (32 * KG) + a.n) * a.Hkv + 7) / 8 * 8;         // ids of either kind begin on the first XCD
     attn_packed_bwd_kernel<HD, KG><<<dim3((unsigned)(kv + slots * a.Hq)), BWD_WAVES * 64, LDS, st>>>(g, (int)kv);
@@ -547,7 +581,11 @@ hipError_t launch_bwd(hipStream_t st, const AttnBwdArgs& b, const PackedShape& a
 //                 20 x 200, 32/8 (408) 80 86;  4 x 2048, 64/8 (544) 971 1010;  3000, 12/12 (288) 145 141; 1541 + 1026 + 400, 16/16
 //                 (416) 78 90
 template <int HD>
-hipError_t launch_hd(hipStream_t st, const AttnBwdArgs& b, const PackedShape& a) {
+hipError_t launch_hd(hipStream_t st, const PackedBwdArgs& b, const PackedShape& a) {
+    const int per_group = 4 * (HD == 64 ? 32 : 16);
+    minus_delta_kernel<HD><<<(unsigned)(((long)a.T * a.Hq + per_group - 1) / per_group), 256, 0, st>>>(b.dO, b.o, b.minus_delta, a.T, a.Hq);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
     const long groups = ((long)a.T / 128 + a.n) * a.Hkv;
     if (HD == 128) return groups <= (a.Hq > a.Hkv ? 400 : 288) ? launch_bwd<HD, 2>(st, b, a) : launch_bwd<HD, 4>(st, b, a);
     if constexpr (HD != 128)
@@ -558,7 +596,7 @@ hipError_t launch_hd(hipStream_t st, const AttnBwdArgs& b, const PackedShape& a)
 
 }  // namespace
 
-hipError_t spk_launch_attention_packed_bwd(hipStream_t st, const AttnBwdArgs& b, const PackedShape& a) {
+hipError_t spk_launch_attention_packed_bwd(hipStream_t st, const PackedBwdArgs& b, const PackedShape& a) {
     switch (a.hd) {
         case 64: return launch_hd<64>(st, b, a);
         case 80: return launch_hd<80>(st, b, a);

@@ -154,7 +154,13 @@ struct PackedShape {
 // lse (nullable) fp32 [Hq, T].
 hipError_t spk_launch_attention_packed(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* lse, const PackedShape& a);
 // g.lse and g.delta fp32 [Hq, T].
-hipError_t spk_launch_attention_packed_bwd(hipStream_t st, const AttnBwdArgs& g, const PackedShape& a);
+struct PackedBwdArgs {
+    const bf16_t *qkv, *o, *dO;
+    const float* lse;
+    float* minus_delta;      // scratch, [Hq][T]
+    bf16_t* dqkv;
+};
+hipError_t spk_launch_attention_packed_bwd(hipStream_t st, const PackedBwdArgs& g, const PackedShape& a);
 
 struct BatchPlanArgs {
     const int *lens, *cached, *free_blocks;   // cached: nullptr = nothing yet

@@ -75,7 +75,7 @@ extern "C" int spk_attention_packed(void* stream, const uint16_t* qkv, const int
 
 extern "C" size_t spk_attention_packed_bwd_scratch_bytes(int T, int Hq) {
     if (T < 1 || T > kMostPositions || Hq < 1) return 0;
-    return ((size_t)T * Hq * 4 + 255) / 256 * 256;     // delta = rowsum(dO * O)
+    return ((size_t)T * Hq * 4 + 255) / 256 * 256;     // -rowsum(dO * O)
 }
 
 extern "C" int spk_attention_packed_bwd(void* stream, const uint16_t* qkv, const int32_t* cu, const uint16_t* o, const uint16_t* dO,
@@ -84,12 +84,8 @@ extern "C" int spk_attention_packed_bwd(void* stream, const uint16_t* qkv, const
     if (any_null({qkv, cu, o, dO, lse, scratch, dqkv}) || misaligned(16, {qkv, o, dO, scratch, dqkv}) || misaligned(4, {cu, lse}) ||
         !packed_ok(n, T, Hq, Hkv, hd))
         return SP_ERR_INVALID_ARG;
-    hipStream_t s = (hipStream_t)stream;
-    float* delta = static_cast<float*>(scratch);
-    hipError_t e = spk_launch_attn_delta(s, dO, o, delta, 1, T, Hq, hd);
-    if (e != hipSuccess) return st(e);
-    AttnBwdArgs g{qkv, dO, lse, delta, dqkv};
-    return st(spk_launch_attention_packed_bwd(s, g, PackedShape{cu, n, T, Hq, Hkv, hd, causal != 0}));
+    return st(spk_launch_attention_packed_bwd((hipStream_t)stream, PackedBwdArgs{qkv, o, dO, lse, static_cast<float*>(scratch), dqkv},
+                                              PackedShape{cu, n, T, Hq, Hkv, hd, causal != 0}));
 }
 
 static bool cache_ok(int blocks, int block_size, int Hq, int Hkv, int hd) {
