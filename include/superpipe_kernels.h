@@ -144,7 +144,8 @@ int spk_colsum_bf16(void* stream, const uint16_t* src, int ld, int T, int n, flo
  * cu[r] .. cu[r+1]-1 of the T rows of a buffer (cu int32 [n+1], ascending, cu[n] <= T; requests without rows are
  * allowed).  cu, lengths, tables and slots are device arrays, so that a step needs nothing from the host and can be captured;
  * int32 and fp32 arrays need the alignment of their type only (scales: 8 bytes).  Whatever those arrays hold, the calls
- * stay inside the buffers they are given.  Rows that belong to no request are left as they were. */
+ * stay inside the buffers they are given.  Rows that belong to no request, also those in front of cu[0], are left as they
+ * were.  Scratch is one call's: calls that may overlap need one each. */
 
 /* One step's bookkeeping: request r, which has cached[r] positions already (cached == NULL: none has), gets lens[r] >= 0 new ones.
  *   cu[0] = 0, cu[r+1] = cu[r] + lens[r];  kv_len[r] = cached[r] + lens[r]           (int32 [n+1], [n])
@@ -165,7 +166,8 @@ int spk_batch_plan(void* stream, const int32_t* lens, const int32_t* cached, con
                    int32_t* info, int n, int block_size);
 
 /* spk_attention inside each request: row i attends the rows of its own request (causal != 0: up to itself).
- * qkv bf16 [T, (Hq+2Hkv)*hd], o bf16 [T, Hq*hd] (not the same memory), lse fp32 [Hq, T] or NULL.  hd in {64,80,128}.
+ * qkv bf16 [T, (Hq+2Hkv)*hd], o bf16 [T, Hq*hd] (not the same memory), lse fp32 [Hq, T] or NULL.  hd in {64,80,128};
+ * Hq <= 16384 and (T / 32 + n) * Hq < 2^22.
  * A tile of 64 keys is worked as a whole: a key or value that is not finite may reach rows of its request up to 63 positions before
  * it; other requests' rows never. */
 int spk_attention_packed(void* stream, const uint16_t* qkv, const int32_t* cu, uint16_t* o, float* lse, int n, int T,
@@ -182,7 +184,7 @@ int spk_attention_packed_bwd(void* stream, const uint16_t* qkv, const int32_t* c
 /* A key/value cache in 8 bits, one layer's: a pool of blocks of block_size (16, 32, 64) tokens,
  *   k8 [blocks][Hkv][block_size][hd], v8 [blocks][Hkv][hd][block_size]: e4m3 (one byte, no infinities);
  *   scales fp32 [blocks][Hkv][2]: what a block's key and value codes are multiplied with, powers of two.
- * hd 64 or 128; blocks * block_size <= 2^31 - 1.
+ * hd 64 or 128; Hq <= 32767; blocks * block_size <= 2^31 - 1.
  *
  * Append: the key and value parts of row t of qkv bf16 [T, (Hq+2Hkv)*hd] go to slot slots[t] (block slots[t] / block_size,
  * position slots[t] % block_size; outside the pool: the row is skipped).  Rows of one block have to lie close together, none more

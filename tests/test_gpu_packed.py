@@ -305,6 +305,39 @@ def test_packed_attention_backward_large():
     check_backward([900, 5], 0, 24, 24, 128, 1)
 
 
+def test_packed_attention_of_the_most_heads():
+    """16384 query heads on one key/value head."""
+    check_forward([1, 2], 0, 16384, 1, 64, 1)
+    check_backward([1, 2], 0, 16384, 1, 64, 1)
+
+
+def test_packed_attention_on_two_streams():
+    """Two batches on two streams at once, several times over: the bits of each alone, forward and backward."""
+    rng = np.random.default_rng(14)
+    calls = []
+    for lens, hq, hkv, hd in (([400, 33, 700], 8, 2, 128), ([90, 1, 513, 64], 8, 8, 64)):
+        T, cu = sum(lens), i32(sums(lens))
+        q, do = dev_u16(rand_bf16(rng, (T, (hq + 2 * hkv) * hd))[0]), dev_u16(rand_bf16(rng, (T, hq * hd), 0.5)[0])
+        o, dx, lse = torch.zeros_like(do), torch.zeros_like(q), torch.zeros((hq, T), device=DEV)
+        scratch = torch.zeros(sp.spk_attention_packed_bwd_scratch_bytes(T, hq), dtype=torch.uint8, device=DEV)
+
+        def call(s, q=q, cu=cu, o=o, lse=lse, do=do, scratch=scratch, dx=dx, n=len(lens), T=T, hq=hq, hkv=hkv, hd=hd):
+            assert sp.spk_attention_packed(s, ptr(q), ptr(cu), ptr(o), ptr(lse), n, T, hq, hkv, hd, 1) == sp.SP_OK
+            assert sp.spk_attention_packed_bwd(s, ptr(q), ptr(cu), ptr(o), ptr(do), ptr(lse), ptr(scratch), ptr(dx), n, T, hq, hkv, hd, 1) == sp.SP_OK
+        call(stream_ptr())
+        torch.cuda.synchronize()
+        calls.append((call, o, dx, o.clone(), dx.clone(), torch.cuda.Stream()))
+    for _, o, dx, _, _, _ in calls:
+        o.zero_(), dx.zero_()
+    torch.cuda.synchronize()
+    for _ in range(6):
+        for call, *_, stream in calls:
+            call(stream.cuda_stream)
+    torch.cuda.synchronize()
+    for _, o, dx, o1, dx1, _ in calls:
+        assert torch.equal(o, o1) and torch.equal(dx, dx1)
+
+
 def test_packed_attention_gradient_against_differences():
     """The kernels' gradient along a direction against differences of the 64-bit forward; the bound is the gradient's own,
     element by element, along that direction, and that of the o and lse which it was given (each off by its rounding:
@@ -517,6 +550,20 @@ def test_cache_attention(bs, hq, hkv, hd):
 def test_cache_attention_in_pieces(lens, bs, hq, hkv, hd, extra):
     """Positions shared out over work-groups; pieces that nobody fills."""
     check_cache_attention(lens, bs, hq, hkv, hd, extra)
+
+
+def test_cache_attention_of_the_most_requests():
+    """65535 requests of at most 20 positions, which share blocks; some of the rows against the oracle."""
+    rng = np.random.default_rng(65)
+    B, bs, blocks = 65535, 16, 50
+    table, lens = rng.integers(0, blocks, (B, 2)).astype(np.int32), rng.integers(0, 21, B)
+    k8, v8, sc = filled(rng, blocks, 1, bs, 64)
+    sc[:] = 2.0 ** -8
+    qbits, q = rand_bf16(rng, (B, 4 * 64), 0.3)
+    got = run_cache_attention(qbits, k8, v8, sc, table, lens, bs, 2, 1, 64)
+    some = np.concatenate([np.arange(40), rng.integers(0, B, 100), B - 1 - np.arange(40)])
+    want, weight = P.kv8_attention(q[some, :128].reshape(-1, 2, 64), k8, v8, sc.astype(np.float64), table[some], lens[some], bs)
+    assert np.all(np.abs(got[some] - want) <= STEP * (weight + np.abs(want)) + FP32 * weight)
 
 
 def test_cache_behind_four_gigabytes():
