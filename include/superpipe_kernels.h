@@ -174,7 +174,8 @@ int spk_attention_packed(void* stream, const uint16_t* qkv, const int32_t* cu, u
                          int Hq, int Hkv, int hd, int causal);
 
 /* Its backward: o and lse as the forward left them, dO bf16 [T, Hq*hd]; dqkv bf16 (layout of qkv) receives dq, dk, dv, the
- * gradients of a key/value head summed over the query heads that share it (fixed order, no atomics).  scratch:
+ * gradients of a key/value head summed over the query heads that share it (fixed order, no atomics); what is not finite may reach
+ * the gradients of rows of its request up to 63 positions off.  scratch:
  * spk_attention_packed_bwd_scratch_bytes bytes (the fp32 row sums of dO * O). */
 size_t spk_attention_packed_bwd_scratch_bytes(int T, int Hq);
 int spk_attention_packed_bwd(void* stream, const uint16_t* qkv, const int32_t* cu, const uint16_t* o, const uint16_t* dO,
