@@ -751,3 +751,40 @@ def test_captured_step_is_the_eager_step():
         eager.free = torch.cat([eager.free[:eager.taken], eager.free[eager.taken + taken:], eager.free[eager.taken:eager.taken + taken]])
         cap.free.copy_(eager.free)
         old.copy_(new)
+
+
+def test_captured_training_step_takes_other_lengths():
+    """Forward and backward captured once, replayed on other lengths and rows, with eager work and synchronizations between the
+    replays: the eager bits."""
+    hq, hkv, hd, T, n = 8, 2, 128, 700, 5
+    rng = np.random.default_rng(44)
+    buf = {}
+    for who in ("eager", "captured"):
+        z = lambda *shape, dtype=torch.int16: torch.zeros(shape, dtype=dtype, device=DEV)  # noqa: E731
+        buf[who] = dict(qkv=z(T, 12 * hd), do=z(T, hq * hd), o=z(T, hq * hd), dx=z(T, 12 * hd), lse=z(hq, T, dtype=torch.float32), cu=z(n + 1, dtype=torch.int32),
+                        scratch=z(sp.spk_attention_packed_bwd_scratch_bytes(T, hq), dtype=torch.uint8))
+
+    def step(b):
+        assert sp.spk_attention_packed(stream_ptr(), ptr(b["qkv"]), ptr(b["cu"]), ptr(b["o"]), ptr(b["lse"]), n, T, hq, hkv, hd, 1) == sp.SP_OK
+        assert sp.spk_attention_packed_bwd(stream_ptr(), ptr(b["qkv"]), ptr(b["cu"]), ptr(b["o"]), ptr(b["do"]), ptr(b["lse"]), ptr(b["scratch"]),
+                                           ptr(b["dx"]), n, T, hq, hkv, hd, 1) == sp.SP_OK
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            step(buf["captured"])
+    torch.cuda.current_stream().wait_stream(side)
+    for lens in ([700, 0, 0, 0, 0], [1, 300, 2, 33, 64], [100, 100, 100, 100, 100], [0, 0, 0, 0, 1]):
+        q, d = dev_u16(rand_bf16(rng, (T, 12 * hd))[0]), dev_u16(rand_bf16(rng, (T, hq * hd), 0.5)[0])
+        for b in buf.values():
+            b["qkv"].copy_(q), b["do"].copy_(d), b["cu"].copy_(i32(sums(lens)))
+            for name in ("o", "dx"):
+                b[name].fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        step(buf["eager"])
+        torch.cuda.synchronize()
+        used = sum(lens)
+        for name in ("o", "dx"):
+            a, b = buf["eager"][name], buf["captured"][name]
+            assert torch.equal(a, b) and bool((a[used:] == 7).all()) and bool((a[:used] != 7).any()), (lens, name)
