@@ -269,6 +269,7 @@ hipError_t launch_append(hipStream_t st, const bf16_t* qkv, const int* slots, in
 // then the B operand as it stands, K and V are read as they lie, and all that a lane weighs belongs to one block -- one
 // key scale, which multiplies its scores, and one value scale, which the conversion applies.
 constexpr int NW8 = 4;
+constexpr float LOWEST = -3.402823466e38f;        // finite: the weight of a score of -inf is then 0
 
 __device__ __forceinline__ bf16x8_t bf16_of_codes(uint32_t a, uint32_t b, float scale) {
     union { bf16x2_t p[4]; bf16x8_t v; } u;
@@ -334,7 +335,8 @@ __global__ __launch_bounds__(NW8 * 64, 3) void kv8_attn_kernel(const bf16_t* __r
     f32x4_t acc[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    float m_run = -3.402823466e38f, l_run = 0.f;
+    float m_run = LOWEST, l_run = 0.f;
+    int seen = 0;                          // this lane has met a position
     constexpr int STEP = NW8 * 64;
     int t0 = s0 + w * 64;
     int ev = entry(t0, g), ek = entry(t0, r >> 2), ek_next = entry(t0 + STEP, r >> 2), ev_next = entry(t0 + STEP, g);
@@ -365,6 +367,7 @@ __global__ __launch_bounds__(NW8 * 64, 3) void kv8_attn_kernel(const bf16_t* __r
         if (more) load_k(t0 + STEP, ek_next);
         const bool ok = (unsigned)ev < (unsigned)c.blocks;
         const int left = ok ? min(max(n - (t0 + 16 * g), 0), 16) : 0;      // positions of this lane's 16
+        seen |= left;
         const float sk = sc.x * scale_log2e, sv = left ? sc.y : 1.0f;
         float mx = -INFINITY;
 #pragma unroll
@@ -414,7 +417,10 @@ __global__ __launch_bounds__(NW8 * 64, 3) void kv8_attn_kernel(const bf16_t* __r
     l_run += __shfl_xor(l_run, 32, 64);
 #pragma unroll
     for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4_t*>(&buf[w][r][t * 16 + 4 * g]) = acc[t];
-    if (g == 0) { wm[w][r] = m_run; wl[w][r] = l_run; }
+    // No positions and no weight are different states: scores that are all -inf leave the lowest finite maximum and a sum of 0, which
+    // gives NaN as the definition does (0 / 0); without positions the maximum is -inf, and if everybody's is, o is 0.
+    const bool met = __any(seen);
+    if (g == 0) { wm[w][r] = met ? m_run : -INFINITY; wl[w][r] = l_run; }
     __syncthreads();
     for (int i = threadIdx.x; i < heads * HD; i += NW8 * 64) {
         const int head = i / HD, d = i % HD;
@@ -422,14 +428,15 @@ __global__ __launch_bounds__(NW8 * 64, 3) void kv8_attn_kernel(const bf16_t* __r
 #pragma unroll
         for (int k = 1; k < NW8; ++k) M = fmaxf(M, wm[k][head]);
         float L = 0.f, a = 0.f;
+        const float top = fmaxf(M, LOWEST);
 #pragma unroll
         for (int k = 0; k < NW8; ++k) {
-            const float f = __builtin_amdgcn_exp2f(wm[k][head] - M);
+            const float f = __builtin_amdgcn_exp2f(wm[k][head] - top);
             L = fmaf(f, wl[k][head], L);
             a = fmaf(f, buf[k][head][d], a);
         }
         if (splits == 1) {
-            o[((size_t)b * Hq + hq + head) * HD + d] = f2bf(L == 0.f ? 0.f : a / L);
+            o[((size_t)b * Hq + hq + head) * HD + d] = f2bf(M == -INFINITY ? 0.f : a / L);
         } else {
             float* pr = part + (((size_t)b * Hq + hq + head) * splits + split) * (HD + 2);
             pr[d] = a;
@@ -452,10 +459,11 @@ __global__ __launch_bounds__(256) void kv8_combine_kernel(const float* __restric
     auto ml_of = [&](int s) { return s < pieces ? *reinterpret_cast<const float2*>(p + (size_t)s * (HD + 2) + HD) : make_float2(-INFINITY, 0.f); };
     float M = -INFINITY, L = 0.f;
     for (int s = lane; s < pieces; s += 64) M = fmaxf(M, ml_of(s).x);
-    M = wave_max(M);                   // finite: a piece's maximum is never below the lowest finite value
+    M = wave_max(M);                   // -inf: no piece has positions
+    const float top = fmaxf(M, LOWEST);
     for (int s = lane; s < pieces; s += 64) {
         const float2 ml = ml_of(s);
-        L = fmaf(__builtin_amdgcn_exp2f(ml.x - M), ml.y, L);
+        L = fmaf(__builtin_amdgcn_exp2f(ml.x - top), ml.y, L);
     }
     L = wave_sum(L);
     float a[E] = {};
@@ -472,10 +480,10 @@ __global__ __launch_bounds__(256) void kv8_combine_kernel(const float* __restric
         for (int k = 0; k < BATCH; ++k)
             if (s0 + NW * k < pieces) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) a[e] = fmaf(__builtin_amdgcn_exp2f(f[k] - M), v[k][e], a[e]);
+                for (int e = 0; e < E; ++e) a[e] = fmaf(__builtin_amdgcn_exp2f(f[k] - top), v[k][e], a[e]);
             }
     }
-    const float inv = L == 0.f ? 0.f : 1.0f / L;
+    const float inv = M == -INFINITY ? 0.f : 1.0f / L;
     if (NW == 1) {
 #pragma unroll
         for (int e = 0; e < E; ++e)

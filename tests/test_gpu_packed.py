@@ -633,6 +633,37 @@ def test_cache_attention_nan_stays_with_its_request():
     assert np.all(np.isnan(got[0, 2:])) and np.array_equal(got[1], clean[1])
 
 
+@pytest.mark.parametrize("hd,hq,hkv,n,bs,width", [
+    (64, 4, 2, 40, 16, 4),              # one piece
+    (128, 4, 2, 900, 64, 16),           # pieces, added up by a wave per head
+    (128, 4, 1, 5000, 64, 80),          # by four
+])
+def test_cache_attention_of_scores_that_are_all_minus_infinity(hd, hq, hkv, n, bs, width):
+    """An infinite query on keys of one sign: 0 / 0, as the definition has it.  Requests without positions give zeros whatever their
+    query is; a stretch of scores of -inf, longer than a piece, weighs nothing beside finite ones."""
+    rng = np.random.default_rng(n)
+    lens, per = [n, n, 0, n], -(-n // bs)
+    table = np.zeros((4, width), np.int32)
+    table[:, :per] = np.arange(4 * per).reshape(4, per)
+    table[0, per:] = -1
+    k8, v8, sc = filled(rng, 4 * per, hkv, bs, hd)
+    sc[:] = 2.0 ** -8
+    k8[:, :, :, 0] = 0xFE                                    # -448: the largest code
+    k8[table[3, per - 1], :, :, 0] = 0                       # request 3: but the last block's
+    qbits, q = rand_bf16(rng, (4, (hq + 2 * hkv) * hd), 0.3)
+    qbits.reshape(4, -1, hd)[:3, 1, 0] = 0x7F80              # head 1 of the others
+    qbits.reshape(4, -1, hd)[3, :hq, 0] = 0x7F7F             # sums that pass fp32: finite in 64 bits, and their weight is 0 there too
+    got = run_cache_attention(qbits, k8, v8, sc, table, lens, bs, hq, hkv, hd)
+    want, weight = P.kv8_attention(bf16_vals(qbits)[:, :hq * hd].reshape(4, hq, hd)[[0, 1, 3]], k8, v8, sc.astype(np.float64), table[[0, 1, 3]],
+                                   [n] * 3, bs)
+    assert not got[2].any()
+    got = got[[0, 1, 3]]
+    assert np.all(np.isnan(got[:2, 1])) and np.all(np.isnan(want[:2, 1]))
+    got[:2, 1] = want[:2, 1] = weight[:2, 1] = 0
+    off = np.abs(got - want) - (STEP * (weight + np.abs(want)) + FP32 * weight)
+    assert off.max() <= 0, float(off.max())
+
+
 # ---- together --------------------------------------------------------------------------------------------
 
 class Server:
