@@ -145,7 +145,8 @@ int spk_colsum_bf16(void* stream, const uint16_t* src, int ld, int T, int n, flo
  * allowed).  cu, lengths, tables and slots are device arrays, so that a step needs nothing from the host and can be captured;
  * int32 and fp32 arrays need the alignment of their type only (scales: 8 bytes).  Whatever those arrays hold, the calls
  * stay inside the buffers they are given.  Rows that belong to no request, also those in front of cu[0], are left as they
- * were.  Scratch is one call's: calls that may overlap need one each. */
+ * were.  Scratch is one call's: calls that may overlap need one each.  What a call writes may lie neither over what it reads
+ * nor over something else that it writes: SP_ERR_INVALID_ARG. */
 
 /* One step's bookkeeping: request r, which has cached[r] positions already (cached == NULL: none has), gets lens[r] >= 0 new ones.
  *   cu[0] = 0, cu[r+1] = cu[r] + lens[r];  kv_len[r] = cached[r] + lens[r]           (int32 [n+1], [n])
@@ -158,15 +159,14 @@ int spk_colsum_bf16(void* stream, const uint16_t* src, int ld, int T, int n, flo
  * What does not fit is not carried out at all: no rows (cu = 0, slots = -1), kv_len = cached, table as it was, and info[3] names
  * the reasons, summed: 1 more rows than max_tokens, 2 more blocks than n_free, 4 a request past max_blocks, 8 a negative
  * length (info[0..2] count all the same, negative lengths as 0).
- * block_size 16, 32 or 64; max_blocks * block_size <= 2^30; 1 <= max_tokens <= 2^30; free_blocks may be NULL with n_free == 0;
- * What the call writes may overlap neither what it reads nor each other (hand cached and kv_len over in turn); an entry of table or
- * free_blocks that is no block number (negative, or too large for a slot) gives slots of -1. */
+ * block_size 16, 32 or 64; max_blocks * block_size <= 2^30; 1 <= max_tokens <= 2^30; free_blocks may be NULL with n_free == 0.
+ * kv_len may not be cached itself: hand two arrays over in turn.  An entry of table or free_blocks that is no block number (negative, or too large for a slot) gives slots of -1. */
 int spk_batch_plan(void* stream, const int32_t* lens, const int32_t* cached, const int32_t* free_blocks, int n_free,
                    int32_t* table, int max_blocks, int32_t* cu, int32_t* kv_len, int32_t* slots, int max_tokens,
                    int32_t* info, int n, int block_size);
 
 /* spk_attention inside each request: row i attends the rows of its own request (causal != 0: up to itself).
- * qkv bf16 [T, (Hq+2Hkv)*hd], o bf16 [T, Hq*hd] (not the same memory), lse fp32 [Hq, T] or NULL.  hd in {64,80,128};
+ * qkv bf16 [T, (Hq+2Hkv)*hd], o bf16 [T, Hq*hd], lse fp32 [Hq, T] or NULL.  hd in {64,80,128};
  * Hq <= 16384 and (T / 32 + n) * Hq < 2^22.
  * A tile of 64 keys is worked as a whole: a key or value that is not finite may reach rows of its request up to 63 positions before
  * it; other requests' rows never. */

@@ -664,6 +664,40 @@ def test_cache_attention_of_scores_that_are_all_minus_infinity(hd, hq, hkv, n, b
     assert off.max() <= 0, float(off.max())
 
 
+def test_arrays_side_by_side():
+    """Inputs and outputs that share one allocation, end to end, are no overlap: the bits of arrays of their own."""
+    rng = np.random.default_rng(17)
+    lens, hq, hkv, hd, bs, blocks = [70, 1, 57], 4, 2, 64, 16, 12
+    T, cu, n = 128, i32(sums(lens)), 3
+    bits, db = rand_bf16(rng, (T, 8 * hd))[0], rand_bf16(rng, (T, hq * hd), 0.5)[0]
+    sizes = [("qkv", bits.nbytes), ("o", db.nbytes), ("dO", db.nbytes), ("lse", 4 * hq * T), ("scratch", 4 * hq * T), ("dqkv", bits.nbytes),
+             ("slots", 4 * T), ("k8", blocks * bs * hkv * hd), ("v8", blocks * bs * hkv * hd), ("scales", blocks * hkv * 8), ("table", 64), ("kv_len", 16),
+             ("step", n * hq * hd * 2)]
+    outs = []
+    for gap in (0, 256):
+        pool = torch.zeros(sum(v + gap for _, v in sizes), dtype=torch.uint8, device=DEV)
+        at, a = 0, {}
+        for name, size in sizes:
+            a[name] = pool[at:at + size]
+            at += size + gap
+        for name, v in (("qkv", bits), ("dO", db), ("slots", np.concatenate([np.arange(70), [80], 96 + np.arange(57)]).astype(np.int32)),
+                        ("table", np.array([[0, 1, 2, 3, 4], [5] * 5, [6, 7, 8, 9, 6]], np.int32)), ("kv_len", np.array([70, 1, 57], np.int32))):
+            v = torch.from_numpy(np.ascontiguousarray(v).view(np.uint8).reshape(-1)).to(DEV)
+            a[name][:v.numel()] = v
+        p = {k: ptr(v) for k, v in a.items()}
+        assert sp.spk_attention_packed(stream_ptr(), p["qkv"], ptr(cu), p["o"], p["lse"], n, T, hq, hkv, hd, 1) == sp.SP_OK
+        assert sp.spk_attention_packed_bwd(stream_ptr(), p["qkv"], ptr(cu), p["o"], p["dO"], p["lse"], p["scratch"], p["dqkv"], n, T, hq, hkv,
+                                           hd, 1) == sp.SP_OK
+        assert sp.spk_kv8_append(stream_ptr(), p["qkv"], p["slots"], p["k8"], p["v8"], p["scales"], T, blocks, bs, hq, hkv, hd) == sp.SP_OK
+        assert sp.spk_kv8_attention_scratch_bytes(n, 5, bs, hq, hkv, hd) == 0
+        assert sp.spk_kv8_attention(stream_ptr(), p["qkv"], p["k8"], p["v8"], p["scales"], p["table"], p["kv_len"], p["step"], None, n, blocks, bs,
+                                    5, hq, hkv, hd) == sp.SP_OK
+        torch.cuda.synchronize()
+        outs.append({k: v.clone() for k, v in a.items()})
+    for name, _ in sizes:
+        assert torch.equal(outs[0][name], outs[1][name]) and bool(outs[0][name].any()), name
+
+
 # ---- together --------------------------------------------------------------------------------------------
 
 class Server:

@@ -119,6 +119,74 @@ def test_cache_refusals():
     assert sp.spk_kv8_plan(2, 4, 16, 4, 3, (C.c_int * 2)()) == BAD and sp.spk_kv8_plan(2, 4, 16, 4, 2, None) == BAD
 
 
+def spread(names):
+    """An address per array, far from one another and never followed: every call with them below ends in the argument checks."""
+    return {name: (i + 1) << 20 for i, name in enumerate(names)}
+
+
+def test_attention_refuses_overlaps():
+    """Outputs over inputs, over one another, by a whole array or by its last bytes."""
+    shape = dict(n=2, T=64, hq=4, hkv=2, hd=64)
+    wide, rows, row_values = 64 * 8 * 64 * 2, 64 * 4 * 64 * 2, 64 * 4 * 4         # bytes of qkv, of o, of lse
+    a = dict(spread(["qkv", "cu", "o", "lse", "dO", "scratch", "dqkv"]), **shape)
+
+    def call(**kw):
+        x = dict(a, **kw)
+        return sp.spk_attention_packed(None, x["qkv"], x["cu"], x["o"], x["lse"], x["n"], x["T"], x["hq"], x["hkv"], x["hd"], 1)
+
+    def call_bwd(**kw):
+        x = dict(a, **kw)
+        return sp.spk_attention_packed_bwd(None, x["qkv"], x["cu"], x["o"], x["dO"], x["lse"], x["scratch"], x["dqkv"], x["n"], x["T"],
+                                           x["hq"], x["hkv"], x["hd"], 1)
+    for kw in (dict(o=a["qkv"]), dict(o=a["qkv"] + wide - 16), dict(o=a["qkv"] - rows + 16), dict(o=a["cu"]), dict(o=a["cu"] - rows + 16),
+               dict(lse=a["qkv"]), dict(lse=a["o"] + rows - 4), dict(lse=a["o"] - row_values + 4), dict(lse=a["cu"] + 8)):
+        assert call(**kw) == BAD, kw
+    for name, size in (("qkv", wide), ("o", rows), ("dO", rows), ("lse", row_values), ("cu", 16)):
+        for kw in (dict(dqkv=a[name]), dict(dqkv=a[name] + size - 16), dict(dqkv=a[name] - wide + 16), dict(scratch=a[name]),
+                   dict(scratch=a[name] + size - 16), dict(scratch=a[name] - row_values + 16)):
+            assert call_bwd(**kw) == BAD, kw
+    for kw in (dict(scratch=a["dqkv"]), dict(scratch=a["dqkv"] + wide - 16), dict(scratch=a["dqkv"] - row_values + 16)):
+        assert call_bwd(**kw) == BAD, kw
+    # what was refused before, by arrays that lie apart
+    for kw in (dict(qkv=None), dict(cu=None), dict(o=None), dict(n=0), dict(n=4097), dict(T=0), dict(T=(1 << 30) + 1), dict(hq=3), dict(hq=0),
+               dict(hkv=0), dict(hq=16386), dict(hd=96), dict(hd=256), dict(qkv=a["qkv"] + 2), dict(o=a["o"] + 8), dict(cu=a["cu"] + 2)):
+        assert call(**kw) == BAD and call_bwd(**kw) == BAD, kw
+    for kw in (dict(dO=None), dict(lse=None), dict(scratch=None), dict(dqkv=None), dict(dqkv=a["dqkv"] + 4), dict(scratch=a["scratch"] + 4)):
+        assert call_bwd(**kw) == BAD, kw
+
+
+def test_cache_refuses_overlaps():
+    shape = dict(T=8, B=8, blocks=4, bs=16, mb=40, hq=4, hkv=2, hd=64)
+    sizes = dict(qkv=8 * 8 * 64 * 2, k8=4 * 16 * 2 * 64, v8=4 * 16 * 2 * 64, scales=4 * 2 * 8, slots=32, table=8 * 40 * 4, kv_len=32, o=8 * 4 * 64 * 2)
+    sizes["scratch"] = sp.spk_kv8_attention_scratch_bytes(8, 40, 16, 4, 2, 64)
+    assert sizes["scratch"] > 0
+    a = dict(spread(sizes), **shape)
+
+    def append(x):
+        return sp.spk_kv8_append(None, x["qkv"], x["slots"], x["k8"], x["v8"], x["scales"], x["T"], x["blocks"], x["bs"], x["hq"],
+                                 x["hkv"], x["hd"])
+
+    def attend(x):
+        return sp.spk_kv8_attention(None, x["qkv"], x["k8"], x["v8"], x["scales"], x["table"], x["kv_len"], x["o"], x["scratch"], x["B"],
+                                    x["blocks"], x["bs"], x["mb"], x["hq"], x["hkv"], x["hd"])
+    for call, written, others in ((append, ("k8", "v8", "scales"), ("qkv", "slots", "k8", "v8", "scales")),
+                                  (attend, ("o", "scratch"), ("qkv", "k8", "v8", "scales", "table", "kv_len", "o", "scratch"))):
+        for w in written:
+            for other in others:
+                if w != other:
+                    for at in (a[other], a[other] + sizes[other] - 16, a[other] - sizes[w] + 16):
+                        assert call(dict(a, **{w: at})) == BAD, (w, other, at - a[other])
+    for kw in (dict(qkv=None), dict(k8=None), dict(v8=None), dict(scales=None), dict(blocks=0), dict(blocks=1 << 27), dict(bs=8), dict(bs=128),
+               dict(hq=3), dict(hkv=0), dict(hd=80), dict(hd=32), dict(qkv=a["qkv"] + 2), dict(k8=a["k8"] + 8), dict(v8=a["v8"] + 1),
+               dict(scales=a["scales"] + 4)):
+        assert append(dict(a, **kw)) == BAD and attend(dict(a, **kw)) == BAD, kw
+    for kw in (dict(slots=None), dict(T=0), dict(T=(1 << 30) + 1), dict(slots=a["slots"] + 2)):
+        assert append(dict(a, **kw)) == BAD, kw
+    for kw in (dict(table=None), dict(kv_len=None), dict(o=None), dict(B=0), dict(B=65536), dict(mb=0), dict(mb=(1 << 26) + 1),
+               dict(table=a["table"] + 2), dict(o=a["o"] + 8), dict(scratch=None)):
+        assert attend(dict(a, **kw)) == BAD, kw
+
+
 def test_kv8_plan_covers_the_table():
     out = (C.c_int * 2)()
     rng = np.random.default_rng(5)
