@@ -33,22 +33,21 @@ __device__ __forceinline__ float half_max(float v) {
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-template <int HD, int NWAVES>
+constexpr int NW = 4;                    // waves of a work-group
+template <int HD>
 struct PackedCfg {
-    static constexpr int NW = NWAVES, MQ = 1, QB = NW * MQ * 32;
     typedef AttnCfg<HD, NW> C;
     static constexpr int STAGES = 2;
     static constexpr int LDS = STAGES * C::STAGE;
     static_assert(LDS <= 160 * 1024, "fits the LDS");
 };
 
-template <int HD, int NW>
+template <int HD>
 __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void attn_packed_kernel(const bf16_t* __restrict__ qkv, const int* __restrict__ cu,
                                                            bf16_t* __restrict__ o, float* __restrict__ lse, int n, int T,
                                                            int Hq, int Hkv, int causal, float scale_log2e) {
-    typedef PackedCfg<HD, NW> G;
-    typedef typename G::C C;
-    constexpr int MQ = G::MQ, QB = G::QB;
+    typedef typename PackedCfg<HD>::C C;
+    constexpr int QB = C::QB;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem_packed[];     // stages of {K tile, V tile}
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, half = lane >> 5;
@@ -97,85 +96,67 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void attn_packed_kernel
     const int vp0 = rowv * C::ROWB + (C::v_swz(rowv) << 6) + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
     auto v_at = [&](int base, int mt) { return smem_packed + (XOR ? (base + vp0) ^ (mt << 6) : base + vp0 + mt * 64); };
 
-    const int q0 = pb.blk * QB, wq0 = q0 + wave * (MQ * 32), qi = wq0 + l32;
-    bf16x8_t qf[MQ][C::NKS];
+    const int q0 = pb.blk * QB, wq0 = q0 + wave * 32, qi = wq0 + l32;
+    bf16x8_t qf[C::NKS];
+    {
+        const bf16_t* qp = qkv + (tok0 + min(qi, len - 1)) * ld + h * HD + half * 8;
 #pragma unroll
-    for (int m = 0; m < MQ; ++m) {
-        const bf16_t* qp = qkv + (tok0 + min(qi + 32 * m, len - 1)) * ld + h * HD + half * 8;
-#pragma unroll
-        for (int ks = 0; ks < C::NKS; ++ks) qf[m][ks] = *reinterpret_cast<const bf16x8_t*>(qp + ks * 16);
+        for (int ks = 0; ks < C::NKS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8_t*>(qp + ks * 16);
     }
-    f32x16_t oacc[MQ][C::NMT];
-    float m_run[MQ], l_run[MQ];
+    f32x16_t oacc[C::NMT];
+    float m_run = -3.402823466e38f, l_run = 0.f;       // finite: a step without a visible key then has probabilities 0
 #pragma unroll
-    for (int m = 0; m < MQ; ++m) {
-        m_run[m] = -3.402823466e38f;       // finite: a step without a visible key then has probabilities 0
-        l_run[m] = 0.f;
-#pragma unroll
-        for (int t = 0; t < C::NMT; ++t)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) oacc[m][t][e] = 0.f;
-    }
+    for (int t = 0; t < C::NMT; ++t) oacc[t] = zeros();
     const int ntiles = ((causal ? min(len, q0 + QB) : len) + KB - 1) / KB;               // of the work-group
-    const int mine = wq0 >= len ? 0 : ((causal ? min(len, wq0 + MQ * 32) : len) + KB - 1) / KB;   // of this wave
+    const int mine = wq0 >= len ? 0 : ((causal ? min(len, wq0 + 32) : len) + KB - 1) / KB;   // of this wave
 
     // Scores of a tile's first 32 keys, nothing beside them: all fragments are on their way before the first MFMA.
-    auto scores = [&](int base, f32x16_t (&s)[MQ]) __attribute__((always_inline)) {
+    auto scores = [&](int base, f32x16_t& s) __attribute__((always_inline)) {
         bf16x8_t kf[C::NKS];
 #pragma unroll
         for (int ks = 0; ks < C::NKS; ++ks) kf[ks] = lds_frag(k_at(base, ks));
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int ks = 0; ks < C::NKS; ++ks)
-#pragma unroll
-            for (int m = 0; m < MQ; ++m) s[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[m][ks], ks ? s[m] : zeros(), 0, 0, 0);
+        for (int ks = 0; ks < C::NKS; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[ks], ks ? s : zeros(), 0, 0, 0);
     };
-    f32x16_t sa[MQ], sb[MQ];
-    float alpha[MQ], mx[MQ];                 // mx: of the lane's 16 scores of the next step
+    f32x16_t sa, sb;
+    float mx;                                // mx: of the lane's 16 scores of the next step
     // Masks the scores of the 32 keys from key0 on, moves the references that they ask for, and rescales what was summed up to them.
-    auto settle = [&](f32x16_t (&s)[MQ], int key0, bool mask) __attribute__((always_inline)) {
-        bool any = false;
+    auto settle = [&](f32x16_t& s, int key0, bool mask) __attribute__((always_inline)) {
+        if (mask) {
+            // element e is key key0 + 4 half + (e >> 2) * 8 + (e & 3)
+            const int last = min(len - 1, causal ? qi : len - 1) - key0 - 4 * half;
 #pragma unroll
-        for (int m = 0; m < MQ; ++m) {
-            if (mask) {
-                // element e is key key0 + 4 half + (e >> 2) * 8 + (e & 3)
-                const int last = min(len - 1, causal ? qi + 32 * m : len - 1) - key0 - 4 * half;
+            for (int e = 0; e < 16; ++e) s[e] = (e >> 2) * 8 + (e & 3) <= last ? s[e] : -INFINITY;
+            mx = s[0];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s[m][e] = (e >> 2) * 8 + (e & 3) <= last ? s[m][e] : -INFINITY;
-                mx[m] = s[m][0];
-#pragma unroll
-                for (int e = 1; e < 16; ++e) mx[m] = fmaxf(mx[m], s[m][e]);
-            }
-            const float top = half_max(mx[m]);
-            // the reference follows the maximum lazily, see k_attn.hip
-            const bool move = (top - m_run[m]) * scale_log2e > 8.0f;
-            const float m_new = move ? top : m_run[m];
-            alpha[m] = move ? __builtin_amdgcn_exp2f((m_run[m] - m_new) * scale_log2e) : 1.0f;
-            m_run[m] = m_new;
-            any |= move;
+            for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
         }
-        if (__any(any)) {
+        const float top = half_max(mx);
+        // the reference follows the maximum lazily, see k_attn.hip
+        const bool move = (top - m_run) * scale_log2e > 8.0f;
+        const float m_new = move ? top : m_run;
+        float alpha = move ? __builtin_amdgcn_exp2f((m_run - m_new) * scale_log2e) : 1.0f;
+        m_run = m_new;
+        if (__any(move)) {
+            asm volatile("" : "+v"(alpha));          // keeps the products here: speculated they cost their time in every step, and 64 registers
+            l_run *= alpha;
 #pragma unroll
-            for (int m = 0; m < MQ; ++m) {
-                float f = alpha[m];
-                asm volatile("" : "+v"(f));          // keeps the products here: speculated they cost their time in every step, and 64 registers
-                l_run[m] *= f;
+            for (int t = 0; t < C::NMT; ++t)
 #pragma unroll
-                for (int t = 0; t < C::NMT; ++t)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) oacc[m][t][e] *= f;
-            }
+                for (int e = 0; e < 16; ++e) oacc[t][e] *= alpha;
         }
     };
     // One step of 32 keys, settled scores s: the next step's scores beside the probabilities of this one, then its output beside
     // the maximum of the next.  The order is the source's: fragments are read PF ahead of the MFMA that takes them, and each
     // MFMA is followed by its share of the vector arithmetic (left to the compiler, every read was waited for at once; the
     // empty asm statements keep it from sinking the arithmetic to its use).
-    auto step = [&](f32x16_t (&s)[MQ], f32x16_t (&s_next)[MQ], int base, int off_v, int off_k, bool next) __attribute__((always_inline)) {
+    auto step = [&](f32x16_t& s, f32x16_t& s_next, int base, int off_v, int off_k, bool next) __attribute__((always_inline)) {
         constexpr int NK = C::NKS, NV = 2 * C::NMT, PF = NK < 5 ? NK : 5;
-        u32x4_t p[MQ][2];
+        u32x4_t p[2];
         bf16x8_t kf[NK], vf[NV];
-        float m_scaled[MQ], sum[MQ];
+        const float m_scaled = m_run * scale_log2e;
+        float sum = 0.f;
         auto kread = [&](int i) __attribute__((always_inline)) { kf[i] = lds_frag(k_at(base, i) + off_k); };
         auto vread = [&](int i) __attribute__((always_inline)) {
             const unsigned char* vp = v_at(base, i % C::NMT) + off_v + 16 * (i / C::NMT) * C::ROWB;
@@ -186,11 +167,6 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void attn_packed_kernel
 #pragma unroll
         for (int i = 0; i < PF; ++i)
             if (next) kread(i);
-#pragma unroll
-        for (int m = 0; m < MQ; ++m) {
-            m_scaled[m] = m_run[m] * scale_log2e;
-            sum[m] = 0.f;
-        }
         // Ahead of the wave that shares the SIMD until half of the output is done: the two then work different parts (2 x 2000
         // tokens, 32/8 heads: 77 us for 83; 64/8 heads over 5241: 274 for 279).  Three waves to a SIMD, at head_dim 64 and 80,
         // lose by it (40 sequences of 52 to 571, 16 heads of 80: 41.6 for 40.9).
@@ -200,42 +176,31 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void attn_packed_kernel
         for (int i = 0; i < NK; ++i) {
             if (i + PF >= NK) vread(i + PF - NK);
             else if (next) kread(i + PF);
+            if (next) s_next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[i], i ? s_next : zeros(), 0, 0, 0);
 #pragma unroll
-            for (int m = 0; m < MQ; ++m)
-                if (next) s_next[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[m][i], i ? s_next[m] : zeros(), 0, 0, 0);
-#pragma unroll
-            for (int m = 0; m < MQ; ++m)
-#pragma unroll
-                for (int e = 8 * i / NK; e < 8 * (i + 1) / NK; ++e) {
-                    const float v = __builtin_amdgcn_exp2f(fmaf(s[m][2 * e], scale_log2e, -m_scaled[m]));
-                    const float w = __builtin_amdgcn_exp2f(fmaf(s[m][2 * e + 1], scale_log2e, -m_scaled[m]));
-                    sum[m] += v + w;
-                    uint32_t pw = __builtin_bit_cast(uint32_t, bf16x2_t{(__bf16)v, (__bf16)w});      // at most 256: half a step of bf16, as every operand of the products
-                    asm volatile("" : "+v"(pw));
-                    p[m][e >> 2][e & 3] = pw;
-                }
+            for (int e = 8 * i / NK; e < 8 * (i + 1) / NK; ++e) {
+                const float v = __builtin_amdgcn_exp2f(fmaf(s[2 * e], scale_log2e, -m_scaled));
+                const float w = __builtin_amdgcn_exp2f(fmaf(s[2 * e + 1], scale_log2e, -m_scaled));
+                sum += v + w;
+                uint32_t pw = __builtin_bit_cast(uint32_t, bf16x2_t{(__bf16)v, (__bf16)w});      // at most 256: half a step of bf16, as every operand of the products
+                asm volatile("" : "+v"(pw));
+                p[e >> 2][e & 3] = pw;
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
-#pragma unroll
-        for (int m = 0; m < MQ; ++m) {
-            l_run[m] += sum[m];
-            mx[m] = s_next[m][0];
-        }
+        l_run += sum;
+        if (next) mx = s_next[0];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if constexpr (HD == 128)
                 if (i == NV / 2) __builtin_amdgcn_s_setprio(0);
             if (i + PF < NV) vread(i + PF);
+            oacc[i % C::NMT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i], __builtin_bit_cast(bf16x8_t, p[i / C::NMT]), oacc[i % C::NMT], 0, 0, 0);
+            if (next) {
 #pragma unroll
-            for (int m = 0; m < MQ; ++m)
-                oacc[m][i % C::NMT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i], __builtin_bit_cast(bf16x8_t, p[m][i / C::NMT]), oacc[m][i % C::NMT], 0, 0, 0);
-#pragma unroll
-            for (int m = 0; m < MQ; ++m)
-                if (next) {
-#pragma unroll
-                    for (int e = 16 * i / NV; e < 16 * (i + 1) / NV; ++e) mx[m] = fmaxf(mx[m], s_next[m][e]);
-                    asm volatile("" : "+v"(mx[m]));
-                }
+                for (int e = 16 * i / NV; e < 16 * (i + 1) / NV; ++e) mx = fmaxf(mx, s_next[e]);
+                asm volatile("" : "+v"(mx));
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -266,12 +231,9 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void attn_packed_kernel
     if (mine > 0) {
         auto begin = [&]() __attribute__((always_inline)) {
             scores((kt & 1) * C::STAGE, sa);
+            mx = sa[0];
 #pragma unroll
-            for (int m = 0; m < MQ; ++m) {
-                mx[m] = sa[m][0];
-#pragma unroll
-                for (int e = 1; e < 16; ++e) mx[m] = fmaxf(mx[m], sa[m][e]);
-            }
+            for (int e = 1; e < 16; ++e) mx = fmaxf(mx, sa[e]);
         };
         begin();
         for (; kt + 1 < mine;) {
@@ -284,25 +246,20 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void attn_packed_kernel
     while (kt + 1 < ntiles) {
         enter(++kt);
     }
+    const float l = l_run + __shfl_xor(l_run, 32, 64);
+    if (qi >= len) return;
+    const float inv = 1.0f / l;
+    bf16_t* op = o + (tok0 + qi) * (size_t)(Hq * HD) + h * HD;
 #pragma unroll
-    for (int m = 0; m < MQ; ++m) {
-        const float l = l_run[m] + __shfl_xor(l_run[m], 32, 64);
-        const int q = qi + 32 * m;
-        if (q >= len) continue;
-        const float inv = 1.0f / l;
-        bf16_t* op = o + (tok0 + q) * (size_t)(Hq * HD) + h * HD;
+    for (int mt = 0; mt < C::NMT; ++mt)
 #pragma unroll
-        for (int mt = 0; mt < C::NMT; ++mt)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int e0 = mt * 32 + g * 8 + half * 4;
-                if (e0 < HD)
-                    *reinterpret_cast<uint2*>(op + e0) =
-                        make_uint2(pack_bf2(oacc[m][mt][g * 4] * inv, oacc[m][mt][g * 4 + 1] * inv),
-                                   pack_bf2(oacc[m][mt][g * 4 + 2] * inv, oacc[m][mt][g * 4 + 3] * inv));
-            }
-        if (lse && half == 0) lse[(size_t)h * T + tok0 + q] = m_run[m] * scale_log2e * 0.69314718055994530942f + logf(l);
-    }
+        for (int g = 0; g < 4; ++g) {
+            const int e0 = mt * 32 + g * 8 + half * 4;
+            if (e0 < HD)
+                *reinterpret_cast<uint2*>(op + e0) = make_uint2(pack_bf2(oacc[mt][g * 4] * inv, oacc[mt][g * 4 + 1] * inv),
+                                                                pack_bf2(oacc[mt][g * 4 + 2] * inv, oacc[mt][g * 4 + 3] * inv));
+        }
+    if (lse && half == 0) lse[(size_t)h * T + tok0 + qi] = m_run * scale_log2e * 0.69314718055994530942f + logf(l);
 }
 
 // The same for batches of few blocks: a work-group has 32 queries of one head and its four waves share out the keys, wave w
@@ -475,14 +432,14 @@ hipError_t launch_split(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* lse
     return hipGetLastError();
 }
 
-template <int HD, int NW>
+template <int HD>
 hipError_t launch_packed(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* lse, const PackedShape& a) {
-    typedef PackedCfg<HD, NW> G;
+    typedef PackedCfg<HD> G;
     static LdsLimitOnce lds_limit;
-    hipError_t e = lds_limit.set(reinterpret_cast<const void*>(attn_packed_kernel<HD, NW>), G::LDS);
+    hipError_t e = lds_limit.set(reinterpret_cast<const void*>(attn_packed_kernel<HD>), G::LDS);
     if (e != hipSuccess) return e;
-    const int slots = a.T / G::QB + a.n;
-    attn_packed_kernel<HD, NW><<<dim3((unsigned)((long)slots * a.Hq)), 64 * G::NW, G::LDS, st>>>(qkv, a.cu, o, lse, a.n, a.T, a.Hq, a.Hkv,
+    const int slots = a.T / G::C::QB + a.n;
+    attn_packed_kernel<HD><<<dim3((unsigned)((long)slots * a.Hq)), 64 * NW, G::LDS, st>>>(qkv, a.cu, o, lse, a.n, a.T, a.Hq, a.Hkv,
                                                                                              a.causal, 1.4426950408889634f / sqrtf((float)HD));
     return hipGetLastError();
 }
@@ -499,7 +456,7 @@ hipError_t launch_hd(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* lse, c
     const long groups = ((long)a.T / 32 + a.n) * a.Hq;
     const bool lengthy = a.T / a.n >= 1000;
     const long most = HD == 80 ? 256 : !lengthy ? 512 : HD == 64 ? 1024 : 768;
-    return groups <= most ? launch_split<HD>(st, qkv, o, lse, a) : launch_packed<HD, 4>(st, qkv, o, lse, a);
+    return groups <= most ? launch_split<HD>(st, qkv, o, lse, a) : launch_packed<HD>(st, qkv, o, lse, a);
 }
 
 }  // namespace
