@@ -201,6 +201,8 @@ int spk_kv8_append(void* stream, const uint16_t* qkv, const int32_t* slots, uint
  * of its row of table int32 [B, max_blocks]; q_b = the query part of row b of qkv bf16 [B, (Hq+2Hkv)*hd].  Positions in
  * blocks outside the pool have weight 0, so have those behind max_blocks; a request without positions gives zeros, one
  * whose scores are all -inf NaN (0 / 0), as in spk_attention_packed.
+ * Values are worked in bf16, which holds code * scale exactly for scales from 2^-124 on (below: rounded to multiples of 2^-133) and up to
+ * 2^128: a bf16 value of 248 * 2^120 or more is stored as 2^128, counts as infinite and gives NaN where its weight is 0.
  * scratch: spk_kv8_attention_scratch_bytes bytes (may be NULL if that is 0); two calls that may overlap need
  * one each.  B <= 65535. */
 size_t spk_kv8_attention_scratch_bytes(int B, int max_blocks, int block_size, int Hq, int Hkv, int hd);

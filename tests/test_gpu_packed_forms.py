@@ -205,3 +205,34 @@ def test_many_heads_without_log_sum_exp_on_two_streams_and_captured(hq, hkv, hd)
         torch.cuda.synchronize()
         for name in ("o", "dx"):
             assert torch.equal(eager[name], cap[name]) and bool((cap[name][sum(lens):] == 7).all()), (lens, name)
+
+
+@pytest.mark.parametrize("e", [-126, -125, -124, -60, 0, 119, 120])
+def test_cache_attention_of_every_code(e):
+    """One position of weight 1: code * scale itself, rounded to multiples of 2^-133 and infinite from 2^128 on."""
+    k8, v8, sc = np.full((4, 1, 16, 64), 0x38, np.uint8), np.full((4, 1, 64, 16), 0x7F, np.uint8), np.ones((4, 1, 2), np.float32)
+    v8[:, 0, :, 0] = np.arange(256).reshape(4, 64)
+    sc[:, :, 1] = 2.0 ** e
+    q = rand_bf16(np.random.default_rng(1), (4, 3 * 64))[0]
+    got = B.run_cache_attention(q, k8, v8, sc, np.arange(4).reshape(4, 1), np.ones(4, int), 16, 1, 1, 64).reshape(256)
+    want = np.round(P.E4M3 * 2.0 ** e * 2.0 ** 133) * 2.0 ** -133
+    want[np.abs(want) >= 2.0 ** 128] *= np.inf
+    assert np.array_equal(got, want, equal_nan=True)
+
+
+@pytest.mark.parametrize("n", [2, 300])
+def test_cache_attention_of_the_largest_values(n):
+    """The largest bf16 values through append and attention, the first position with all the weight: 248 * 2^120 and more are stored as
+    2^128 and count as infinite, NaN where they weigh nothing; under that the element is what the first position holds."""
+    hd, bs, blocks = 64, 16, 20
+    bits = np.zeros((n, 3 * hd), np.uint16)
+    x = bits.reshape(n, 3, hd)
+    x[0, 1], x[1:, 1] = 0x4100, 0xC100                        # keys 8 and -8
+    x[:, 2] = 0x3F80                                          # values 1
+    x[1, 2, :8] = [0x7F60, 0x7F70, 0x7F77, 0x7F78, 0x7F7F, 0xFF7F, 0xFF77, 0x7F00]
+    k8, v8, sc = B.run_append(bits, np.arange(n), *B.filled(np.random.default_rng(2), blocks, 1, bs, hd), bs, 1, 1, hd)
+    q = np.full((1, 3 * hd), 0x4100, np.uint16)
+    got = B.run_cache_attention(q, k8, v8, sc, np.arange(blocks).reshape(1, -1), np.array([n]), bs, 1, 1, hd)[0, 0]
+    assert sc[0, 0, 1] == 2.0 ** 120 and list(v8[0, 0, 3:6, 1]) == [0x78, 0x78, 0xF8]
+    assert np.all(np.isnan(got[3:6]))
+    assert not np.any(got[[0, 1, 2, 6, 7]]) and not np.any(got[8:])      # 1 is code 0 at that scale
