@@ -1,8 +1,10 @@
 /*
- * superpipe_kernels.h -- C ABI test hooks for the individual per-layer kernels.
+ * superpipe_kernels.h -- C ABI of the individual kernels.
  *
- * These exist so that each kernel can be compared with the CPU oracle's op on
- * its own; the product path is superpipe.h.  All pointers are device (HBM)
+ * The per-layer ones are test hooks: each can be compared with the CPU oracle's
+ * op on its own, the product path of the stacks is superpipe.h.  The operators
+ * of the last section, "packed batches", are for a caller's own steps: no call
+ * of superpipe.h runs them.  All pointers are device (HBM)
  * addresses on the current HIP device, 16-byte aligned; `stream` is a
  * hipStream_t (NULL = default stream).  Calls enqueue and return a sp_status
  * (SP_ERR_INVALID_ARG when the shape is one the kernel does not take,
@@ -142,7 +144,10 @@ int spk_colsum_bf16(void* stream, const uint16_t* src, int ld, int T, int n, flo
 /* ---- packed batches: requests of different lengths ----
  * A batch of n requests (1 <= n <= 4096) has its rows one behind the other: request r has the rows
  * cu[r] .. cu[r+1]-1 of the T rows of a buffer (cu int32 [n+1], ascending, cu[n] <= T; requests without rows are
- * allowed).  cu, lengths, tables and slots are device arrays, so that a step needs nothing from the host and can be captured;
+ * allowed).  cu, lengths, tables and slots are device arrays, so that a call needs nothing from the host and can be captured
+ * and replayed for other contents.  Which kernels run and how work is cut follows from T, n and max_blocks, not from those contents:
+ * buffers far larger than the batch cost time (prompts of 500 and 300 rows, 8 heads of 128: 9 us, 15 with T 8000 rows larger; 2 requests
+ * of 3000 cached positions, 32/8 heads of 128: 9 us, 12 with a table 40 times as wide).
  * int32 and fp32 arrays need the alignment of their type only (scales: 8 bytes).  Whatever those arrays hold, the calls
  * stay inside the buffers they are given.  Rows that belong to no request, also those in front of cu[0], are left as they
  * were.  Scratch is one call's: calls that may overlap need one each.  What a call writes may lie neither over what it reads
@@ -160,7 +165,8 @@ int spk_colsum_bf16(void* stream, const uint16_t* src, int ld, int T, int n, flo
  * the reasons, summed: 1 more rows than max_tokens, 2 more blocks than n_free, 4 a request past max_blocks, 8 a negative
  * length (info[0..2] count all the same, negative lengths as 0).
  * block_size 16, 32 or 64; max_blocks * block_size <= 2^30; 1 <= max_tokens <= 2^30; free_blocks may be NULL with n_free == 0.
- * kv_len may not be cached itself: hand two arrays over in turn.  An entry of table or free_blocks that is no block number (negative, or too large for a slot) gives slots of -1. */
+ * kv_len may not be cached itself: hand two arrays over in turn.  Free blocks are taken from the front of the list; what is left
+ * has to stand there when the call is made, or a captured one replayed, the next time.  An entry of table or free_blocks that is no block number (negative, or too large for a slot) gives slots of -1. */
 int spk_batch_plan(void* stream, const int32_t* lens, const int32_t* cached, const int32_t* free_blocks, int n_free,
                    int32_t* table, int max_blocks, int32_t* cu, int32_t* kv_len, int32_t* slots, int max_tokens,
                    int32_t* info, int n, int block_size);
@@ -190,15 +196,18 @@ int spk_attention_packed_bwd(void* stream, const uint16_t* qkv, const int32_t* c
  * Append: the key and value parts of row t of qkv bf16 [T, (Hq+2Hkv)*hd] go to slot slots[t] (block slots[t] / block_size,
  * position slots[t] % block_size; outside the pool: the row is skipped).  Rows of one block have to lie close together, none more
  * than 64 rows behind the one before it, which they do as spk_batch_plan deals them; they are stored in runs of
- * consecutive slots, in the order of the rows.  A block's scale is the smallest 2^e,
- * e >= -126, with all its finite |x| <= 448 * 2^e; a run that begins inside a block keeps what lies in front of it, re-coded
- * if the scale has to grow, and what lies behind it in the block counts as empty.  Values are rounded to the nearest
+ * consecutive slots, in the order of the rows.  A run that begins at a block's first position gives it the smallest scale 2^e,
+ * e >= -126, with all finite |x| <= 448 * 2^e; one that begins further on keeps what lies in front of it, re-coded
+ * if the scale has to grow (it never falls there, whatever set it), and what lies behind it in the block counts as empty.  Values are rounded to the nearest
  * code, ties to even; infinities and NaN are stored as NaN. */
 int spk_kv8_append(void* stream, const uint16_t* qkv, const int32_t* slots, uint8_t* k8, uint8_t* v8, float* scales, int T,
                    int blocks, int block_size, int Hq, int Hkv, int hd);
 
 /* o bf16 [B, Hq*hd]: row b = softmax(q_b K^T / sqrt(hd)) V over the first kv_len[b] positions of request b, which lie in the blocks
- * of its row of table int32 [B, max_blocks]; q_b = the query part of row b of qkv bf16 [B, (Hq+2Hkv)*hd].  Positions in
+ * of its row of table int32 [B, max_blocks]; q_b = the query part of row b of qkv bf16 [B, (Hq+2Hkv)*hd].  One row per request:
+ * the rows that spk_batch_plan deals lie so only where every request gets exactly one; where some get none or several, the caller
+ * gathers the rows that ask.  (Several new rows of a request that has positions already can be planned and appended; no call
+ * here attends from all of them over the cache.)  Positions in
  * blocks outside the pool have weight 0, so have those behind max_blocks; a request without positions gives zeros, one
  * whose scores are all -inf NaN (0 / 0), as in spk_attention_packed.
  * Values are worked in bf16, which holds code * scale exactly for scales from 2^-124 on (below: rounded to multiples of 2^-133) and up to
