@@ -1,7 +1,7 @@
 // Block tables and slot maps of a batch of requests from their lengths (spk_batch_plan).
 //
-// Prefix sums over the requests, then one lookup per new token.  What bounds it is latency: a few hundred kilobytes are
-// written at the most, and launches and dependent steps are what there is to save.  So it is one launch, without a
+// Prefix sums over the requests, then one lookup per new token.  What bounds it is latency: a server's step writes
+// some hundred kilobytes (4 bytes a row and a new block), and launches and dependent steps are what there is to save.  So it is one launch, without a
 // hand-over between work-groups: every work-group computes the sums over all requests itself (n <= kPackedMaxSeqs lengths,
 // which it reads through the L2), keeps them in LDS and then writes its own share of the tokens, of the requests and of
 // the new table entries.  A block that a request gets by this call is read from the free list by whoever needs its

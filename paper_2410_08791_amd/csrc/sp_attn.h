@@ -17,11 +17,11 @@ struct AttnCfg {
     static constexpr int STAGE = 2 * TILE_BYTES;           // K tile, then V tile
     static constexpr int NINST = STAGE / 1024;             // 1 KiB load instructions per stage
     static constexpr int NLOAD = (NINST + NW - 1) / NW;    // per wave (the last wave may have fewer)
-    // head_dim 80: the rows 80..95 of the third O^T tile are padding.  The V tiles' padding
+    // head_dim 80: the rows 80..95 of the third O^T tile are padding.  In k_attn.hip the V tiles' padding
     // elements are set to 1.0 once and never loaded over, so row 80 of O^T accumulates the sum of
     // the (bf16) probabilities: the softmax denominator comes out of the matrix pipe, which idles
-    // most of the time here, instead of 32 additions per lane and tile on the vector pipe, which
-    // is the one that bounds this kernel.
+    // most of the time there, instead of 32 additions per lane and tile on the vector pipe, which
+    // is the one that bounds that kernel.  (k_attn_packed.hip loads zeros there and sums the unrounded probabilities.)
     static constexpr bool ONES_ROW = HDP > HD;
     static_assert(STAGE % 1024 == 0 && TILE_BYTES % 1024 == 0, "whole load instructions per tile");
     static_assert(HDP * 2 <= ROWB, "the fragment reads of a padded head_dim stay inside the row");
@@ -30,7 +30,7 @@ struct AttnCfg {
     __device__ static int v_swz(int row) { return HD == 128 ? (row & 3) : HD == 64 ? ((row >> 1) & 1) : 0; }
 };
 
-// A 64-row token tile in LDS: rows of ROWB bytes (head_dim 80: 192, the padding is never loaded), the 16-byte
+// A 64-row token tile in LDS: rows of ROWB bytes (head_dim 80: 192; the padding holds nothing that counts: k_attn_bwd.hip never loads it, the packed kernels load zeros), the 16-byte
 // chunk c of row r at position c ^ swz(r).  swz serves both readers: the 16 rows of a straight 16-byte read
 // fall on all banks, and the four consecutive rows of a transposing read in different 64-byte blocks.  It has
 // period 16 in r, and r + 8 flips exactly bit 1 (the hi half of a transposed fragment: address ^ 32).

@@ -153,7 +153,7 @@ struct PackedShape {
 };
 // lse (nullable) fp32 [Hq, T].
 hipError_t spk_launch_attention_packed(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* lse, const PackedShape& a);
-// g.lse and g.delta fp32 [Hq, T].
+// g.lse fp32 [Hq, T]; g.minus_delta takes -rowsum(dO * O).
 struct PackedBwdArgs {
     const bf16_t *qkv, *o, *dO;
     const float* lse;

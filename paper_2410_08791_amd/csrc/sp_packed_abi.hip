@@ -25,7 +25,7 @@ static bool any_null(std::initializer_list<const void*> ptrs) {
     return false;
 }
 
-constexpr int kMostPositions = 1 << 30;      // of a request, and rows of a packed batch: sums of a few of them fit an int
+constexpr int kMostPositions = 1 << 30;      // of a request, and rows of a packed batch: one and a stride of a grid, or a piece, fit an int
 
 // The bytes of an array; NULL meets nothing.
 struct Bytes {
