@@ -5,9 +5,11 @@
 // of a 32-key step), and the probabilities in bf16 are the B operand of O^T = V^T P^T as they stand; tiles of 64 keys come
 // by LDS-DMA and V^T out of the transposing LDS read.
 //
-// What bounds such a kernel: a 32-query wave reads 1 KB of LDS per MFMA of 32 cycles, which for the four SIMDs of a CU is all
-// that its LDS delivers, and the softmax arithmetic takes as many cycles on the vector pipe as the products take on the
-// matrix pipe.
+// What bounds such a kernel: the softmax arithmetic takes as many cycles on the vector pipe as the products take on the matrix pipe (at
+// head_dim 64 nearly twice as many), and the two or three waves of a SIMD do not hide one behind the other.  No unit is full: over
+// 5241 tokens, 64/8 heads of 128, the matrix pipes are busy in 48 % of the cycles, vector instructions issue in 55 %, the LDS
+// works in 24 % (it reads 256 bytes a cycle, a wave needs 1 KB per MFMA of 32); 3 x 3000, 32/8 heads of 64: 38, 72 and 19 %; 40
+// images, 16 heads of 80: 25, 56 and 13 %.
 //
 // The denominator is the fp32 sum of the unrounded probabilities, so that the log-sum-exp is as exact as fp32 allows.  A
 // row of scores that are all -inf gives NaN, as the definition does (0 / 0).
@@ -445,12 +447,16 @@ hipError_t launch_packed(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* ls
 }
 
 // Shared-out keys while the 32-query groups are few: one per CU at head_dim 80, two else, and some more where the sequences are
-// long on average (their first blocks have few keys under a causal mask).  us, 128 queries and 32 (groups of 32):
-//   head_dim 64:  5 prompts of 1 to 128 tokens, 4 heads (56) 5.4 4.2;  3000 tokens, 4 heads (376) 39.7 19.8;  2 x 1000, 16 heads
-//                 (1024) 17.9 16.4;  30 x 100, 8 heads (984) 6.7 8.2;  3000, 16 heads (1504) 43.1 43.5
-//   head_dim 80:  257 tokens, 16 heads (144) 9.2 6.2;  4 x 257 (576) 9.6 16.3
-//   head_dim 128: 2 x 1000, 8 heads (512) 23.6 16.1;  3000, 8 heads (752) 61.2 47.0;  3 x 500, 16 heads (784) 15.1 18.8;
-//                 3000, 16 heads (1504) 64.2 82.0
+// long on average (their first blocks have few keys under a causal mask).  us, 128 queries and 32 (groups of 32), inputs in the
+// caches / out of memory:
+//   head_dim 64:  5 prompts of 1 to 128 tokens, 4 heads (56) 5.9 4.6 / 5.8 4.4;  3000 tokens, 4 heads (376) 40 20 / 40 21;  2 x 1000,
+//                 16 heads (1024) 17.7 16.8 / 18.3 21.8;  30 x 100, 8 heads (984) 6.5 9.8 / 7.5 11.0;  3000, 16 heads (1504) 42 41 / 42 48
+//   head_dim 80, no mask:  257 tokens, 16 heads (144) 9.6 6.6 / 9.8 6.9;  4 x 257 (576) 9.9 16.5 / 10.6 17.4
+//   head_dim 128: 2 x 1000, 8 heads (512) 24 17 / 25 20;  3000, 8 heads (752) 60 45 / 60 47;  3 x 500, 16 heads (784) 15.6 19.4 / 17.1 23.0;
+//                 3000, 16 heads (1504) 64 80 / 66 85
+// Out of memory, over some 250 shapes each (1 to 8 sequences of 64 to 3000, 128 to 1536 groups), the choice costs 1.7 % on average at head_dim
+// 64, 2 (causal) and 4 at 128, 1.7 (no mask) and 8 (causal) at 80 against always the quicker form.  It loses most under a causal mask at
+// head_dim 80 with few long sequences, up to 2.2 times, and with a mean length just over 1000, where the bound rises at once.
 template <int HD>
 hipError_t launch_hd(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* lse, const PackedShape& a) {
     const long groups = ((long)a.T / 32 + a.n) * a.Hq;

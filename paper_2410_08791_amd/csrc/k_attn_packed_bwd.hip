@@ -5,10 +5,11 @@
 //   dq    -- a work-group owns 128 queries of one head and walks the keys.
 // P = exp(s - lse), dS = P (dP - delta), dP = dO V^T (in dk/dv its sums begin at -delta); layouts and tiles are those of k_attn_bwd.hip.
 //
-// What bounds it: 7 products of 2 hd flops per pair of a query and a key on the matrix pipe, 1 KB of LDS and more per MFMA of
-// 32 cycles, and the arithmetic of P and dS on the vector pipe.  At head_dim 128 the eight waves of a CU take 40 KB each out of
-// LDS for the 32 MFMAs of 32 keys and 32 queries in dk/dv (the keys have no room in registers): 2560 cycles of LDS beside 2048
-// of the matrix pipes, of some 3600 that such a step takes.  Batches of few long sequences wait for their longest chain.  Every
+// What bounds it: 7 products of 2 hd flops per pair of a query and a key on the matrix pipe and the arithmetic of P and dS on the
+// vector pipe, in chains that two waves per SIMD do not fill; batches of few long sequences wait for their longest one.  No unit is
+// full.  At head_dim 128 the eight waves of a CU take 40 KB each out of LDS for the 32 MFMAs of 32 keys and 32 queries in dk/dv (the keys
+// have no room in registers), 1280 cycles of LDS beside 2048 of the matrix pipes; over 12 documents, 16 heads of 128, the matrix
+// pipes are busy in 38 % of the cycles, the LDS in 24, vector instructions issue in 33; 9 documents, 32/8 heads of 64: 25, 16 and 35 %.  Every
 // wave therefore reads its fragments a few MFMAs ahead, in an order that the source fixes, and works P beside the MFMAs
 // of dP, and dS beside those of dV (dk/dv) or of the next 32 keys' scores (dq).  One launch: a short batch has too few
 // blocks of either kind to fill the chip.  Four waves each, two work-groups per CU: with one of eight, nothing covered
@@ -572,14 +573,14 @@ hipError_t launch_bwd(hipStream_t st, const PackedBwdArgs& b, const PackedShape&
 
 // Keys of a dk/dv work-group.  Its chain is the queries of all heads that share them, 32 at a time: with 128 keys per group that
 // is what a batch of few groups waits for, with fewer the waves share out the queries and the chain is a half or a quarter.
-// But each group loads all queries.  us for 128, 64, 32 keys (groups of 128 keys in brackets):
-//   head_dim 64:  900 + 200 tokens, 8/4 heads (40) 53.5 30.3 21.4;  3 x 2000, 8/2 (98) 211 115 85;  3000, 8/8 (192) 84 58 69;
-//                 8 x 512, 16/16 (640) 45.3 44.7 55.3;  12 x 300, 32/32 (1280) 58.7 61.2 81.0
-//   head_dim 80:  1500 + 300, 8/2 (32) 161 91 58;  6 x 700, 32/8 (304) 125 97 149;  8 x 577, 16/16 (704) 60.9 63.9 112.6; 4 x 1000,
-//                 8/8 (280), where the chain is one head, 42.5 45.1 61.7
-//   head_dim 128: 3 x 2000, 8/2 (98) 274 174;  3000, 8/8 (192) 118 93;  4000, 32/8 (256) 615 444;  6 x 700, 32/8 (304) 134 125;
-//                 20 x 200, 32/8 (408) 80 86;  4 x 2048, 64/8 (544) 971 1010;  3000, 12/12 (288) 145 141; 1541 + 1026 + 400, 16/16
-//                 (416) 78 90
+// But each group loads all queries.  us for 128, 64, 32 keys under a causal mask, inputs in the caches (groups of 128 keys in brackets):
+//   head_dim 64:  900 + 200 tokens, 8/4 heads (40) 52 30 22;  3 x 2000, 8/2 (98) 198 108 80;  3000, 8/8 (192) 80 58 68;
+//                 8 x 512, 16/16 (640) 42.2 42.5 52.8;  12 x 300, 32/32 (1280) 57 61 83
+//   head_dim 80:  1500 + 300, 8/2 (32) 160 89 57;  6 x 700, 32/8 (304) 103 92 146;  8 x 577, 16/16 (704) 59 63 112; 4 x 1000,
+//                 8/8 (280), where the chain is one head, 41 46 62
+//   head_dim 128: 3 x 2000, 8/2 (98) 266 165;  3000, 8/8 (192) 114 91;  4000, 32/8 (256) 607 438;  6 x 700, 32/8 (304) 131 127;
+//                 20 x 200, 32/8 (408) 80 85;  4 x 2048, 64/8 (544) 984 1009;  3000, 12/12 (288) 127 118; 1541 + 1026 + 400, 16/16
+//                 (416) 77 85
 template <int HD>
 hipError_t launch_hd(hipStream_t st, const PackedBwdArgs& b, const PackedShape& a) {
     const int per_group = 4 * (HD == 64 ? 32 : 16);

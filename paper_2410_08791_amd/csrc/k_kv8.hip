@@ -241,7 +241,11 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(const bf16_t* __restric
 
 template <int HD, int BS>
 hipError_t launch_append_bs(hipStream_t st, const bf16_t* qkv, const int* slots, int T, int Hq, const Kv8Cache& c) {
-    // A wave per row while few rows are left over for a wave, or the rows are too few for work-groups of 64 to fill the chip.
+    // The host cannot tell single tokens, which want a wave per row (a work-group of 64 rows works their blocks four at a time), from
+    // prompts, which want the work-group: few (row, head) pairs are taken for the former.  us by rows and by work-groups of 64 rows, pairs
+    // times two in brackets:  single tokens, 64 of 32 heads of 128 (4096) 5.9 41, 256 (16384) 19 48, 512 of 32 heads of 64
+    // (32768) 24 49;  prompts of 8 heads of 128, 300 tokens (4800) 8.8 4.7, 1000 (16000) 12.0 5.6, 1500 (24000) 12.1 6.0;
+    // 300 tokens, 32 heads of 128, blocks of 16 (19200) 7.3 8.7.
     const bool wave_per_row = (long)T * c.Hkv * 2 <= 16384;
     if (wave_per_row) kv8_append_kernel<HD, BS, 1><<<dim3((unsigned)((T + 3) / 4), c.Hkv * 2), 256, 0, st>>>(qkv, slots, T, Hq, c);
     else kv8_append_kernel<HD, BS, 64><<<dim3((unsigned)((T + 63) / 64), c.Hkv * 2), 256, 0, st>>>(qkv, slots, T, Hq, c);
@@ -446,7 +450,9 @@ __global__ __launch_bounds__(NW8 * 64, 3) void kv8_attn_kernel(const bf16_t* __r
 }
 
 // o from the pieces of a request's positions: NW waves share out the pieces of a head, eight rows in flight each (one chain
-// of dependent loads per piece took 31 us for 59 pieces), and add up in wave order.
+// of dependent loads per piece took 31 us for 59 pieces), and add up in wave order.  Four waves per head from 17 pieces on: up to
+// 16 it makes no difference of 3 % either way, for 24 pieces attention and combination take 12.1 us instead of 12.3, for 40 15.2 instead
+// of 16.5, for 63 8.3 instead of 10.7 (32 heads of 128; 63: 4 of 64).
 template <int HD, int NW>
 __global__ __launch_bounds__(256) void kv8_combine_kernel(const float* __restrict__ part, const int* __restrict__ kv_len,
                                                           bf16_t* __restrict__ o, int splits, int per, int most, int Hq) {
@@ -501,8 +507,12 @@ __global__ __launch_bounds__(256) void kv8_combine_kernel(const float* __restric
 
 // Pieces of 768 positions where that is three rounds of work-groups and more (three live on a CU), of 512 where it fills the
 // chip, else of 256; none where the heads alone fill the chip and nobody has more than 1024 positions (the second launch
-// would cost more).  us without the combination's 4 to 5, 64 requests of 300 to 6000 positions with 8 heads of 128 in pieces of
-// 256, 512, 768, 1024, 1536: 66.1 58.8 57.6 59.0 61.7;  30011 and 17003 positions: 20.5 19.2 20.0 19.4 23.3.
+// would cost more).  The table's width stands for the lengths, which the host does not know.  us without the combination's 4 to 5, 64
+// requests of 300 to 6000 positions with 8 heads of 128 in pieces of 256, 512, 768, 1024, 1536: 66.1 58.8 57.6 59.0 61.7;  30011 and
+// 17003 positions: 20.5 19.2 20.0 19.4 23.3.  With it, tables as wide as the lengths, the rule's choice first:  4 x 2000, 8 heads of 128, 256
+// 9.5, 512 10.6, 1024 13.5;  16 x 2000 256 20.7, 512 18.9, 1024 19.2;  4 x 20000 512 36.7, 256 40.4, 1024 37.5;  64 x 700, 32 heads 1024 64.8,
+// 256 74.1;  64 x 1000, 8 heads of 64 1024 15.0, 512 18.1.  It loses where one piece is enough and the heads do not fill the chip (500
+// positions, 8 heads: 256 7.1, 512 5.7;  32 x 1000, 8 heads: 256 20.8, 1024 16.2) and in the largest batches (32 x 8000: 768 105.9, 1536 99.4).
 struct Kv8Plan { int splits, per; };
 
 Kv8Plan plan_kv8(int B, int max_blocks, int block_size, int Hq, int Hkv) {
