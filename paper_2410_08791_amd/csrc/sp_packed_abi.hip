@@ -27,13 +27,13 @@ static bool any_null(std::initializer_list<const void*> ptrs) {
 
 constexpr int kMostPositions = 1 << 30;      // of a request, and rows of a packed batch: one and a stride of a grid, or a piece, fit an int
 
-// The bytes of an array; NULL meets nothing.
+// The bytes of an array; NULL, or none, meets nothing.
 struct Bytes {
     const void* p;
     size_t n;
     bool meets(const Bytes& o) const {
         const uintptr_t a = (uintptr_t)p, b = (uintptr_t)o.p;
-        return p && o.p && a < b + o.n && b < a + n;
+        return p && o.p && n && o.n && a < b + o.n && b < a + n;
     }
 };
 

@@ -207,6 +207,27 @@ def test_many_heads_without_log_sum_exp_on_two_streams_and_captured(hq, hkv, hd)
             assert torch.equal(eager[name], cap[name]) and bool((cap[name][sum(lens):] == 7).all()), (lens, name)
 
 
+def test_arrays_of_no_bytes_overlap_nothing():
+    """A scratch that the call does not need and an empty free list may point anywhere, also into arrays of the call."""
+    rng = np.random.default_rng(3)
+    hq, hkv, hd, bs = 2, 1, 64, 16
+    k8, v8, sc = B.filled(rng, 4, hkv, bs, hd)
+    q, k, v, s = dev_u16(rand_bf16(rng, (2, 4 * hd))[0]), B.u8(k8), B.u8(v8), dev_f32(sc)
+    t, n, o = B.i32([[0, 1], [2, 3]]), B.i32([20, 32]), torch.zeros((2, hq * hd), dtype=torch.int16, device=DEV)
+    assert sp.spk_kv8_attention_scratch_bytes(2, 2, bs, hq, hkv, hd) == 0
+    outs = []
+    for scratch in (None, ptr(q[1:]), ptr(o.reshape(-1)[64:])):
+        o.zero_()
+        assert sp.spk_kv8_attention(stream_ptr(), ptr(q), ptr(k), ptr(v), ptr(s), ptr(t), ptr(n), ptr(o), scratch, 2, 4, bs, 2, hq, hkv, hd) == sp.SP_OK
+        torch.cuda.synchronize()
+        outs.append(o.clone())
+    assert bool(outs[0].any()) and torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+    lens, cached, cu, kv, slots, info = (B.i32(x) for x in ([1, 2], [3, 4], [0] * 3, [0] * 2, [0] * 3, [0] * 4))
+    assert sp.spk_batch_plan(stream_ptr(), ptr(lens), ptr(cached), ptr(t[1:]), 0, ptr(t), 2, ptr(cu), ptr(kv), ptr(slots), 3, ptr(info), 2, bs) == sp.SP_OK
+    torch.cuda.synchronize()
+    assert slots.tolist() == [3, 2 * bs + 4, 2 * bs + 5] and kv.tolist() == [4, 6]
+
+
 @pytest.mark.parametrize("e", [-126, -125, -124, -60, 0, 119, 120])
 def test_cache_attention_of_every_code(e):
     """One position of weight 1: code * scale itself, rounded to multiples of 2^-133 and infinite from 2^128 on."""
