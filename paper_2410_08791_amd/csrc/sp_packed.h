@@ -15,7 +15,8 @@ struct PackedBlock {
 // most keys) before the others, and so on down to the shortest, so that work-groups start in about the order of their
 // work and the chip empties evenly; the slots left over end at once.  (In the order of the rows the backward took 109 us for
 // 105 over 12 sequences, 16 heads of 128, and 52.8 for 51.8 over 9, 32/8 heads of 64; 40 sequences under no mask took the
-// same.)  The whole wave looks: one load of cu -- each further dependent load would cost every work-group the better part
+// same.  With many short sequences the search costs more than the order brings: 60 of 20 to 400 rows, 32/8 heads of 128, forward 117 us and
+// backward 278, 105 and 268 in the order of the rows; 16 heads of 64 40.4 and 119, 39.0 and 106.)  The whole wave looks: one load of cu -- each further dependent load would cost every work-group the better part
 // of a microsecond -- then lane r adds up the blocks of the sequences in front of sequence r.
 //
 // More: in the order of the rows.  Sequence r owns the slots cu[r] / QB + r .. cu[r + 1] / QB + r, at least ceil(len / QB)
