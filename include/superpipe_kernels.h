@@ -166,7 +166,8 @@ int spk_colsum_bf16(void* stream, const uint16_t* src, int ld, int T, int n, flo
  * length (info[0..2] count all the same, negative lengths as 0).
  * block_size 16, 32 or 64; max_blocks * block_size <= 2^30; 1 <= max_tokens <= 2^30; free_blocks may be NULL with n_free == 0.
  * kv_len may not be cached itself: hand two arrays over in turn.  Free blocks are taken from the front of the list; what is left
- * has to stand there when the call is made, or a captured one replayed, the next time.  An entry of table or free_blocks that is no block number (negative, or too large for a slot) gives slots of -1. */
+ * has to stand there when the call is made, or a captured one replayed, the next time.  An entry of table or
+ * free_blocks that is no block number (negative, or too large for a slot) gives slots of -1. */
 int spk_batch_plan(void* stream, const int32_t* lens, const int32_t* cached, const int32_t* free_blocks, int n_free,
                    int32_t* table, int max_blocks, int32_t* cu, int32_t* kv_len, int32_t* slots, int max_tokens,
                    int32_t* info, int n, int block_size);
@@ -198,8 +199,8 @@ int spk_attention_packed_bwd(void* stream, const uint16_t* qkv, const int32_t* c
  * than 64 rows behind the one before it, which they do as spk_batch_plan deals them; they are stored in runs of
  * consecutive slots, in the order of the rows.  A run that begins at a block's first position gives it the smallest scale 2^e,
  * e >= -126, with all finite |x| <= 448 * 2^e; one that begins further on keeps what lies in front of it, re-coded
- * if the scale has to grow (it never falls there, whatever set it), and what lies behind it in the block counts as empty.  Values are rounded to the nearest
- * code, ties to even; infinities and NaN are stored as NaN. */
+ * if the scale has to grow (it never falls there, whatever set it), and what lies behind it in the block counts as empty.
+ * Values are rounded to the nearest code, ties to even; infinities and NaN are stored as NaN. */
 int spk_kv8_append(void* stream, const uint16_t* qkv, const int32_t* slots, uint8_t* k8, uint8_t* v8, float* scales, int T,
                    int blocks, int block_size, int Hq, int Hkv, int hd);
 
@@ -207,9 +208,9 @@ int spk_kv8_append(void* stream, const uint16_t* qkv, const int32_t* slots, uint
  * of its row of table int32 [B, max_blocks]; q_b = the query part of row b of qkv bf16 [B, (Hq+2Hkv)*hd].  One row per request:
  * the rows that spk_batch_plan deals lie so only where every request gets exactly one; where some get none or several, the caller
  * gathers the rows that ask.  (Several new rows of a request that has positions already can be planned and appended; no call
- * here attends from all of them over the cache.)  Positions in
- * blocks outside the pool have weight 0, so have those behind max_blocks; a request without positions gives zeros, one
- * whose scores are all -inf NaN (0 / 0), as in spk_attention_packed.
+ * here attends from all of them over the cache.)
+ * Positions in blocks outside the pool have weight 0, so have those behind max_blocks; a request without positions gives zeros,
+ * one whose scores are all -inf NaN (0 / 0), as in spk_attention_packed.
  * Values are worked in bf16, which holds code * scale exactly for scales from 2^-124 on (below: rounded to multiples of 2^-133) and up to
  * 2^128: a bf16 value of 248 * 2^120 or more is stored as 2^128, counts as infinite and gives NaN where its weight is 0.
  * scratch: spk_kv8_attention_scratch_bytes bytes (may be NULL if that is 0); two calls that may overlap need
